@@ -136,6 +136,75 @@ mw_status mw_kv_pool_gather(const mw_kv_pool *pool, const int32_t *d_block_table
                             int32_t n_tokens, void *d_k_out, void *d_v_out, mw_stream stream);
 
 /* ------------------------------------------------------------------------
+ * KV pool in 4 bits.  The same pages, block tables and allocator calls
+ * (mw_kv_pool_{set_free_order,alloc,free,num_free,destroy}); the rows are kept
+ * as four-bit floats (one sign, two exponent and one mantissa bit: magnitudes 0,
+ * 0.5, 1, 1.5, 2, 3, 4, 6) with one power of two for each 32 consecutive dims of
+ * a (token, kv head) row: 136 bytes of K and V instead of 512.
+ *   value = code * 2^e,  e the smallest integer with max|x| <= 7 * 2^e over the
+ *   32, kept in [-100, 100]; code the nearest to x * 2^-e, ties to the even
+ *   mantissa, at most 6.
+ * A block that holds an infinity or a NaN reads back as NaN.
+ * A call for one kind of pool refuses the other (MW_ERR_INVALID_ARG).
+ *
+ *   d_k_codes  [num_pages][num_kv_heads][16 tokens][64] bytes: dim 2i in the
+ *              low half of byte i, dim 2i+1 in the high half
+ *   d_v_codes  [num_pages][num_kv_heads][4][16][8][2] bytes: token 4g + 2k + n,
+ *              dim 32 (t / 2) + 2c + t % 2 in half n (0: low) of byte [g][c][t][k]
+ *   d_scales   [num_pages][num_kv_heads][2: K, V][4 blocks][16 tokens] bytes,
+ *              e + 127 (255: not finite)
+ * all 16-byte aligned.  Codes: sign in bit 3, magnitude's index in bits 0-2. */
+mw_status mw_kv4_pool_create(const mw_kv_pool_desc *desc, void *d_k_codes, void *d_v_codes, void *d_scales,
+                             mw_kv_pool **out);
+/* Appends rows, as mw_kv_pool_write does (arguments and checks alike).  Bytes of
+ * V codes hold two tokens each: calls that run at the same time may not write
+ * tokens of one page. */
+mw_status mw_kv4_pool_write(const mw_kv_pool *pool, int32_t batch, const int32_t *h_new_lens,
+                            const int32_t *h_start_pos, const int32_t *d_qo_indptr, const int32_t *d_start_pos,
+                            const int32_t *d_block_table, int32_t bt_stride, const void *d_k_new, const void *d_v_new,
+                            mw_stream stream, mw_timing *timing);
+/* Reads rows back as bf16 (exactly the values held): positions h_start_pos[b] + i,
+ * i < h_lens[b], of each sequence into rows d_indptr[b] + i of d_k_out and d_v_out
+ * (each [num_kv_heads][head_dim]).  Arguments as the write's; rows on a page
+ * outside the pool read as zeros. */
+mw_status mw_kv4_pool_gather(const mw_kv_pool *pool, int32_t batch, const int32_t *h_lens, const int32_t *h_start_pos,
+                             const int32_t *d_indptr, const int32_t *d_start_pos, const int32_t *d_block_table,
+                             int32_t bt_stride, void *d_k_out, void *d_v_out, mw_stream stream, mw_timing *timing);
+
+/* ------------------------------------------------------------------------
+ * Queries and keys between projection and attention: RMS norm of every head,
+ * position rotation, and the append, in one pass.  For each head row x of a
+ * token at position t (its slot in the cache: h_start_pos[b] + i):
+ *     y = x * w / sqrt(mean(x^2) + eps)     (w NULL: y = x)
+ *     (a, c) -> (a cos(t f_i) - c sin(t f_i), c cos(t f_i) + a sin(t f_i))
+ * over the pairs i < rot_dim / 2 of y: (y[i], y[i + rot_dim/2]), or
+ * (y[2i], y[2i+1]) with `neighbours`; dims from rot_dim on are left.  Computed
+ * in fp32 (the angle's product in fp64), rounded to bf16 once.  Queries go to
+ * d_q_out, keys and the values (unchanged) to the pool, which may be of either
+ * kind: in 4 bits the rounded key is what is quantised. */
+typedef struct {
+    int32_t num_q_heads;      /* any >= 0; 0: keys and values only               */
+    int32_t rot_dim;          /* dims that are rotated: a multiple of 16, 0..128 */
+    int32_t neighbours;       /* 0: halves are paired, else neighbours           */
+    float eps;                /* >= 0 and finite                                 */
+    const void *d_q_weight;   /* device bf16 [head_dim], 16-B aligned, or NULL   */
+    const void *d_k_weight;
+    const double *d_inv_freq; /* device [rot_dim / 2]: f_i, radians per position */
+} mw_norm_rope;
+/* Lengths, positions and table as mw_kv_pool_write.  Rows of a token:
+ *   d_q + token * q_stride, [num_q_heads][head_dim] bf16, and so d_k and d_v with
+ *   [num_kv_heads][head_dim]; strides in elements, multiples of 8, no less than a
+ *   token's heads (so the three may be parts of one projection's row); 16-B aligned
+ *   d_q_out [sum n][num_q_heads][head_dim] bf16, dense; may be d_q itself where
+ *   q_stride is num_q_heads * head_dim, and overlap no other input
+ * Queries are written also where the block table maps no page. */
+mw_status mw_qk_norm_rope_write(const mw_kv_pool *pool, const mw_norm_rope *rope, int32_t batch,
+                                const int32_t *h_new_lens, const int32_t *h_start_pos, const int32_t *d_qo_indptr,
+                                const int32_t *d_start_pos, const int32_t *d_block_table, int32_t bt_stride,
+                                const void *d_q, int64_t q_stride, const void *d_k, int64_t k_stride, const void *d_v,
+                                int64_t v_stride, void *d_q_out, mw_stream stream, mw_timing *timing);
+
+/* ------------------------------------------------------------------------
  * CU partition (Sec. 3.2.1: bind each phase's stream to its own compute
  * units; Sec. 5: hipExtStreamCreateWithCUMask on AMD GPUs).
  * MI355X has 8 XCDs of 32 CUs and dispatches workgroups round-robin over the
@@ -349,6 +418,30 @@ mw_status mw_decode_attn_noalloc(const mw_kv_pool *pool, const mw_attn_shape *sh
                                  const int32_t *h_seq_lens, const int32_t *d_seq_lens,
                                  const int32_t *d_block_table, int32_t bt_stride, const void *d_q,
                                  void *d_out, int32_t chunk_pages, mw_stream stream);
+
+/* Attention over a pool in 4 bits: the calls above on the values that the codes
+ * stand for.  K is used as held; queries, probabilities and sums as in the bf16
+ * calls.
+ * Decode: arguments as mw_decode_attn, with its balanced split (chunk_pages 0). */
+mw_status mw_kv4_decode_workspace_size(const mw_attn_shape *shape, int32_t batch, const int32_t *h_seq_lens,
+                                       size_t *bytes);
+mw_status mw_kv4_decode_attn(const mw_kv_pool *pool, const mw_attn_shape *shape, int32_t batch,
+                             const int32_t *h_seq_lens, const int32_t *d_seq_lens, const int32_t *d_block_table,
+                             int32_t bt_stride, const void *d_q, void *d_out, void *d_workspace, size_t workspace_bytes,
+                             mw_stream stream, mw_timing *timing);
+/* Prefill: arguments as mw_prefill_attn_ws.  The batch's pages are unpacked to
+ * bf16 in the workspace and attended there (a chunk of n tokens reads every page
+ * for each of its query blocks).  The workspace is the size call's for these
+ * lengths: 2 * 4096 bytes per (page, kv head) of the batch, a table, and what
+ * mw_prefill_attn_ws takes for itself; layers that run one after the other can
+ * share it. */
+mw_status mw_kv4_prefill_workspace_size(const mw_attn_shape *shape, int32_t batch, const int32_t *h_new_lens,
+                                        const int32_t *h_prefix_lens, int32_t num_cus, size_t *bytes);
+mw_status mw_kv4_prefill_attn(const mw_kv_pool *pool, const mw_attn_shape *shape, int32_t batch,
+                              const int32_t *h_new_lens, const int32_t *h_prefix_lens, const int32_t *d_qo_indptr,
+                              const int32_t *d_prefix_lens, const int32_t *d_block_table, int32_t bt_stride,
+                              const void *d_q, void *d_out, void *d_workspace, size_t workspace_bytes, mw_stream stream,
+                              mw_timing *timing);
 
 /* ------------------------------------------------------------------------ *
  * Contention-tolerant estimator (paper Sec. 3.3) and the prefill-layer count

@@ -231,11 +231,13 @@ mw_status plan_decode(const mw_attn_shape *shape, int32_t batch, const int32_t *
 
 namespace mw {
 
-mw_status decode_prepare(const mw_decode_args *a, int64_t cus, DecodePlan *p, const char *who) {
+mw_status decode_prepare(const mw_decode_args *a, int64_t cus, DecodePlan *p, const char *who, bool four_bit) {
     if (!a || !a->pool || a->bt_stride < 1) return fail(MW_ERR_INVALID_ARG, "%s: bad pool or bt_stride", who);
+    mw_status st = check_pool_kind(a->pool, four_bit, who);
+    if (st != MW_OK) return st;
     const mw_attn_shape *shape = &a->shape;
     Plan pl;
-    mw_status st = plan_decode(shape, a->batch, a->h_seq_lens, a->chunk_pages, a->bt_stride, cus, &pl, who);
+    st = plan_decode(shape, a->batch, a->h_seq_lens, a->chunk_pages, a->bt_stride, cus, &pl, who);
     if (st != MW_OK) return st;
     if (!(shape->scale > 0.f) || !(shape->scale < INFINITY))
         return fail(MW_ERR_INVALID_ARG, "%s: scale must be positive and finite", who);
@@ -264,6 +266,13 @@ mw_status decode_prepare(const mw_decode_args *a, int64_t cus, DecodePlan *p, co
     p->group = shape->num_q_heads / shape->num_kv_heads;
     p->scale_log2 = shape->scale * kLog2e;
     return MW_OK;
+}
+
+uint32_t next_decode_tag() {
+    static std::atomic<uint32_t> last{0};
+    uint32_t t = 0;
+    while (t == 0) t = last.fetch_add(1, std::memory_order_relaxed) + 1;
+    return t;
 }
 
 mw_status decode_combine_launch(const mw_decode_args *a, const DecodePlan &p, hipStream_t s) {
@@ -295,15 +304,6 @@ mw_status mw_decode_workspace_size(const mw_attn_shape *shape, int32_t batch, co
 
 namespace {
 
-// Tag of a balanced-split launch, never 0 (the cleared flag value): a done
-// flag in a workspace counts only for the launch whose tag it shows.
-std::atomic<uint32_t> g_decode_tag{0};
-uint32_t next_tag() {
-    uint32_t t = 0;
-    while (t == 0) t = g_decode_tag.fetch_add(1, std::memory_order_relaxed) + 1;
-    return t;
-}
-
 // The launches of one planned decode call: the balanced split (which merges
 // its own segments), or the fixed-chunk split and its combine.
 mw_status decode_launch(const mw_decode_args &a, const DecodePlan &pl, hipStream_t s, mw_timing *timing) {
@@ -321,7 +321,7 @@ mw_status decode_launch(const mw_decode_args &a, const DecodePlan &pl, hipStream
                                pool->k, pool->v, static_cast<const uint16_t *>(d_q), static_cast<uint16_t *>(d_out),
                                d_seq_lens, d_block_table, bt_stride, reinterpret_cast<float *>(ws),
                                reinterpret_cast<float2 *>(ws + pl.off_ml),
-                               reinterpret_cast<uint32_t *>(ws + pl.off_meta), next_tag(), pl.slots,
+                               reinterpret_cast<uint32_t *>(ws + pl.off_meta), next_decode_tag(), pl.slots,
                                batch, pl.hkv, pl.group, pool->desc.num_pages, pl.scale_log2,
                                static_cast<int>(pl.per_unit), static_cast<int>(pl.total), pl.aligned ? 1 : 0);
             st = check_launch("k_decode_balanced");

@@ -86,7 +86,7 @@ __device__ inline int chunks_of(int L, int ch_pages, int bt_stride) {
 
 // Wave-level search for the sequence b and chunk c holding global chunk ci
 // (every wave runs it; no barrier).  Returns false if ci is past the end.
-__device__ bool locate_chunk(const int32_t *__restrict__ seq_lens, int batch, int ch_pages, int bt_stride,
+__device__ inline bool locate_chunk(const int32_t *__restrict__ seq_lens, int batch, int ch_pages, int bt_stride,
                              int ci, int &b_out, int &c_out, int &nch_out, int &first_out) {
     const int lane = threadIdx.x & 63;
     int running = 0;
@@ -408,13 +408,16 @@ struct alignas(16) Fragment {
     int pad;
 };
 
-struct SpanLds {
-    char buf[kSpanWaves][kSpanBufBytes];    // K/V of the pair in work; at the end the wave's last fragment's O
-    char head[kSpanWaves][kSpanHeadBytes];  // the wave's first fragment's O
-    float m[kSpanWaves][2][16], l[kSpanWaves][2][16];  // [first, last fragment]
+// kBuf, kHead: bytes of a wave's buffers; kHeads: most query heads of a kv head.
+template <int kBuf, int kHead, int kHeads>
+struct SpanLdsOf {
+    char buf[kSpanWaves][kBuf];    // K/V of the pair in work; at the end the wave's last fragment's O
+    char head[kSpanWaves][kHead];  // the wave's first fragment's O
+    float m[kSpanWaves][2][kHeads], l[kSpanWaves][2][kHeads];  // [first, last fragment]
     Fragment frag[kSpanWaves * 2];          // [2 wave + (0: first, 1: last)]
     int done[2];                            // the pending segments' pieces are all done
 };
+using SpanLds = SpanLdsOf<kSpanBufBytes, kSpanHeadBytes, 16>;
 
 // Inclusive scan over the wave's lanes.
 __device__ inline int lane_scan(int x) {
@@ -510,9 +513,11 @@ __device__ __forceinline__ bool locate_page(Lengths &len, int hkv, int align, in
 // heads, and one head per wave of 4 with 8 pieces in flight 24 us for 43
 // pieces of 8 heads).
 constexpr int kMergeAhead = 16;
+template <class Lds>
 __device__ __forceinline__ void
 merge_segment(uint16_t *__restrict__ out, const float *__restrict__ ws_o, const float2 *__restrict__ ws_ml,
-              int64_t first, int nch, int b, int hkv, int kvh, int group, int tid, SpanLds &lds) {
+              int64_t first, int nch, int b, int hkv, int kvh, int group, int tid, Lds &lds) {
+    static_assert(sizeof(lds.buf) >= kSpanThreads * sizeof(float2), "the shares' sums");
     const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     float2 *s_acc = reinterpret_cast<float2 *>(lds.buf);  // [wave][lane]
     const int per_head = group == 1 ? 8 : group == 2 ? 4 : group <= 4 ? 2 : 1;  // waves
@@ -608,10 +613,11 @@ struct Pending {
     int n;  // pieces: 0, 1 or 2
     Piece p0, p1;
 };
+template <class Lds>
 __device__ __forceinline__ void
 finish_segments(uint16_t *__restrict__ out, const float *__restrict__ ws_o, const float2 *__restrict__ ws_ml,
                 uint32_t *__restrict__ flags, uint32_t tag, const Pending &pend, int64_t slots, int hkv, int group,
-                int tid, SpanLds &lds) {
+                int tid, Lds &lds) {
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // this wave's piece stores are complete
     __syncthreads();
     const auto in_workspace = [&](const Pending::Piece &p) {
@@ -648,6 +654,161 @@ finish_segments(uint16_t *__restrict__ out, const float *__restrict__ ws_o, cons
         if (i == 1 && all0) __syncthreads();  // the first merge is done with the LDS
         merge_segment(out, ws_o, ws_ml, p.first, p.nch, p.b, hkv, p.kvh, group, tid, lds);
     }
+}
+
+// A wave's share of a unit's pages, given out in chunks of up to 64 consecutive
+// pages of one segment.
+struct SpanShare {
+    struct Chunk {
+        int b, kvh, p, p_end, np, len, first;
+        bool valid;
+    };
+    const int32_t *bt;
+    int bt_stride, hkv, batch, lane;
+    Lengths len;
+    int b, np, kvh, off, seg_len, seg_first, left;  // left: pages of the share not yet given to a chunk
+
+    __device__ __forceinline__ SpanShare(const int32_t *seq_lens, const int32_t *bt_, int bt_stride_, int batch_, int hkv_,
+                                         int per_unit, int total, bool aligned, int u, int wave, int lane_)
+        : bt(bt_), bt_stride(bt_stride_), hkv(hkv_), batch(batch_), lane(lane_), len{seq_lens, batch_, bt_stride_, 0, 0},
+          b(0), np(0), kvh(0), off(0), seg_len(0), seg_first(0), left(0) {
+        const int align = aligned ? per_unit : 0;
+        // this wave's share [g, g_end) and where it starts
+        const int u0 = u * per_unit;
+        int u1 = min(u0 + per_unit, total);
+        int base = 0, nv = 1;
+        auto at_page = [&](int g) __attribute__((always_inline)) {
+            if (!locate_page(len, hkv, align, g, b, base)) return false;
+            seg_len = len.at(b);
+            np = Lengths::pages(seg_len);
+            nv = aligned ? (np + align - 1) / align * align : np;
+            kvh = (g - base) / nv;
+            seg_first = base + kvh * nv;
+            off = g - seg_first;
+            return true;
+        };
+        bool live = u0 < u1;
+        if (aligned && live) {
+            live = at_page(u0);
+            u1 = u0 + min(per_unit, np - off);  // the padding holds no pages
+        }
+        const int share = (u1 - u0 + kSpanWaves - 1) / kSpanWaves;
+        const int g = u0 + wave * share;
+        left = live ? min(share, u1 - g) : 0;
+        if (aligned)
+            off += wave * share;
+        else if (left > 0 && !at_page(g))
+            left = 0;
+    }
+    __device__ __forceinline__ Chunk next() {
+        Chunk c{b, kvh, off, off, np, seg_len, seg_first, left > 0};
+        if (!c.valid) return c;
+        const int n = min(min(left, np - off), 64);
+        c.p_end = off + n;
+        left -= n;
+        off += n;
+        if (off == np && left > 0) {  // on to the next segment
+            off = 0;
+            seg_first += np;
+            if (++kvh == hkv) {
+                kvh = 0;
+                if (++b < batch) {
+                    seg_len = len.at(b);
+                    np = Lengths::pages(seg_len);
+                } else {
+                    np = 0;
+                }
+                if (np == 0) left = 0;  // device lengths that disagree with the host's
+            }
+        }
+        return c;
+    }
+    __device__ __forceinline__ int table(const Chunk &c) const {  // lane i: page of c.p + i
+        return bt[static_cast<size_t>(c.b) * bt_stride + min(c.p + lane, c.np - 1)];
+    }
+};
+
+// The end of a unit, after the barrier behind its waves' shares: adds up the
+// fragments that they left in LDS, writes out the segments that the unit holds
+// whole and leaves the others' sums as pieces in the workspace.
+template <class Lds>
+__device__ __forceinline__ void
+add_up_fragments(uint16_t *__restrict__ out, float *__restrict__ ws_o, float2 *__restrict__ ws_ml,
+                 uint32_t *__restrict__ flags, uint32_t tag, int64_t slots, int hkv, int group, bool aligned, int u,
+                 int tid, Lds &lds) {
+    const int lane = tid & 63, hq = hkv * group;
+    // The fragments in wave order, each wave's first before its last: those of
+    // one segment are neighbours.  Lane i holds record i, so finding them is
+    // scalar work
+    const Fragment fr = lds.frag[lane & (2 * kSpanWaves - 1)];
+    const bool mine = lane < 2 * kSpanWaves && fr.seg >= 0;
+    uint32_t todo = static_cast<uint32_t>(__builtin_amdgcn_ballot_w64(mine));
+    const uint32_t valid = todo, starts_at = static_cast<uint32_t>(__builtin_amdgcn_ballot_w64(mine && fr.starts)),
+                   ends_at = static_cast<uint32_t>(__builtin_amdgcn_ballot_w64(mine && fr.ends));
+    Pending pend{};
+    while (todo) {
+        // the run: record i and the first fragments of the waves after it
+        const int i = __builtin_ctz(todo), w = i >> 1;
+        int j = i, n = 1;
+        while (!(ends_at >> j & 1) && (j | 1) + 1 < 2 * kSpanWaves && (valid >> ((j | 1) + 1) & 1)) {
+            j = (j | 1) + 1;
+            ++n;
+        }
+        todo &= ~((2u << j) - 1);
+        const bool whole = (starts_at >> i & 1) && (ends_at >> j & 1);
+        const int seg = __builtin_amdgcn_readlane(fr.seg, i);
+        const int sb = __builtin_amdgcn_readlane(fr.b, i), skvh = __builtin_amdgcn_readlane(fr.kvh, i);
+        const int64_t shift = aligned ? 0 : seg;  // of the workspace slots
+        const int64_t piece = u + shift;
+        for (int idx = tid; idx < group * kHeadDim; idx += kSpanThreads) {
+            const int h = idx / kHeadDim, d = idx % kHeadDim;
+            float mk[kSpanWaves], lk[kSpanWaves], ok[kSpanWaves];
+#pragma unroll
+            for (int k = 0; k < kSpanWaves; ++k) {
+                mk[k] = -INFINITY;
+                lk[k] = ok[k] = 0.f;
+                if (k < n) {
+                    const int s = k == 0 ? i & 1 : 0;
+                    mk[k] = lds.m[w + k][s][h];
+                    lk[k] = lds.l[w + k][s][h];
+                    ok[k] = reinterpret_cast<const float *>(s ? lds.buf[w + k] : lds.head[w + k])[h * OSTR + d];
+                }
+            }
+            float M = mk[0];
+#pragma unroll
+            for (int k = 1; k < kSpanWaves; ++k) M = fmaxf(M, mk[k]);
+            float lsum = 0.f, o = 0.f;
+#pragma unroll
+            for (int k = 0; k < kSpanWaves; ++k) {
+                const float wt = mk[k] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mk[k] - M);  // no keys on valid pages
+                lsum += wt * lk[k];
+                o += wt * ok[k];
+            }
+            if (whole) {
+                out[(static_cast<size_t>(sb) * hq + skvh * group + h) * kHeadDim + d] = to_bf16(o / lsum);
+            } else if (piece < slots) {
+                // device-scope stores (through the L2 of this XCD): the piece may be
+                // merged by a work-group on another XCD without a cache writeback
+                __hip_atomic_store(&ws_o[(static_cast<size_t>(piece) * group + h) * kHeadDim + d], o, __ATOMIC_RELAXED,
+                                   __HIP_MEMORY_SCOPE_AGENT);
+                if (d == 0)
+                    __hip_atomic_store(reinterpret_cast<unsigned long long *>(&ws_ml[static_cast<size_t>(piece) * group + h]),
+                                       __builtin_bit_cast(unsigned long long, make_float2(M, lsum)), __ATOMIC_RELAXED,
+                                       __HIP_MEMORY_SCOPE_AGENT);
+            }
+        }
+        if (!whole) {
+            const int64_t f0 = __builtin_amdgcn_readlane(fr.u0, i);
+            const Pending::Piece pc{sb, skvh, __builtin_amdgcn_readlane(fr.nch, i), f0 + shift, piece};
+            if (pend.n == 0)
+                pend.p0 = pc;
+            else
+                pend.p1 = pc;
+            pend.n = pend.n == 0 ? 1 : 2;
+        }
+    }
+    if (pend.n > 0)
+        finish_segments(out, ws_o, ws_ml, flags, tag, pend, slots, hkv, group, tid, lds);
 }
 
 // One unit (work-group) of the balanced split: global pages [u R, min((u + 1) R,
@@ -687,66 +848,10 @@ decode_span(const uint16_t *__restrict__ kpool, const uint16_t *__restrict__ vpo
     const int col = lane & 15, grp = lane >> 4;
     const int hq = hkv * group;
     const int align = aligned ? per_unit : 0;
-    Lengths len{seq_lens, batch, bt_stride, 0, 0};
-
-    // this wave's share [g, g_end) and where it starts
-    const int u0 = u * per_unit;
-    int u1 = min(u0 + per_unit, total);
-    int b = 0, base = 0, np = 0, nv = 1, kvh = 0, off = 0, seg_len = 0, seg_first = 0;
-    auto at_page = [&](int g) __attribute__((always_inline)) {
-        if (!locate_page(len, hkv, align, g, b, base)) return false;
-        seg_len = len.at(b);
-        np = Lengths::pages(seg_len);
-        nv = aligned ? (np + align - 1) / align * align : np;
-        kvh = (g - base) / nv;
-        seg_first = base + kvh * nv;
-        off = g - seg_first;
-        return true;
-    };
-    bool live = u0 < u1;
-    if (aligned && live) {
-        live = at_page(u0);
-        u1 = u0 + min(per_unit, np - off);  // the padding holds no pages
-    }
-    const int share = (u1 - u0 + kSpanWaves - 1) / kSpanWaves;
-    const int g = u0 + wave * share;
-    int left = live ? min(share, u1 - g) : 0;  // pages of the share not yet given to a chunk
-    if (aligned)
-        off += wave * share;
-    else if (left > 0 && !at_page(g))
-        left = 0;
-
-    // ---- the wave's chunks: up to 64 consecutive pages of one segment
-    struct Chunk {
-        int b, kvh, p, p_end, np, len, first;
-        bool valid;
-    };
-    auto next_chunk = [&]() __attribute__((always_inline)) {
-        Chunk c{b, kvh, off, off, np, seg_len, seg_first, left > 0};
-        if (!c.valid) return c;
-        const int n = min(min(left, np - off), 64);
-        c.p_end = off + n;
-        left -= n;
-        off += n;
-        if (off == np && left > 0) {  // on to the next segment
-            off = 0;
-            seg_first += np;
-            if (++kvh == hkv) {
-                kvh = 0;
-                if (++b < batch) {
-                    seg_len = len.at(b);
-                    np = Lengths::pages(seg_len);
-                } else {
-                    np = 0;
-                }
-                if (np == 0) left = 0;  // device lengths that disagree with the host's
-            }
-        }
-        return c;
-    };
-    auto table = [&](const Chunk &c) __attribute__((always_inline)) {  // lane i: page of c.p + i
-        return bt[static_cast<size_t>(c.b) * bt_stride + min(c.p + lane, c.np - 1)];
-    };
+    SpanShare walk{seq_lens, bt, bt_stride, batch, hkv, per_unit, total, aligned, u, wave, lane};
+    using Chunk = SpanShare::Chunk;
+    auto next_chunk = [&]() __attribute__((always_inline)) { return walk.next(); };
+    auto table = [&](const Chunk &c) __attribute__((always_inline)) { return walk.table(c); };
     // Q^T operand: column `col` is query head kvh*group + col.  Columns past
     // the group are zero here, and their reference maximum of +inf makes their
     // probabilities zero too: multiplying zeros draws less power, which the
@@ -952,79 +1057,7 @@ decode_span(const uint16_t *__restrict__ kpool, const uint16_t *__restrict__ vpo
         }
     }
     __syncthreads();
-
-    // ---- add up the fragments of each segment (in wave order, each wave's
-    // first before its last; those of one segment are neighbours).  Lane i
-    // holds record i, so finding them is scalar work
-    const Fragment fr = lds.frag[lane & (2 * kSpanWaves - 1)];
-    const bool mine = lane < 2 * kSpanWaves && fr.seg >= 0;
-    uint32_t todo = static_cast<uint32_t>(__builtin_amdgcn_ballot_w64(mine));
-    const uint32_t valid = todo, starts_at = static_cast<uint32_t>(__builtin_amdgcn_ballot_w64(mine && fr.starts)),
-                   ends_at = static_cast<uint32_t>(__builtin_amdgcn_ballot_w64(mine && fr.ends));
-    Pending pend{};
-    while (todo) {
-        // the run: record i and the first fragments of the waves after it
-        const int i = __builtin_ctz(todo), w = i >> 1;
-        int j = i, n = 1;
-        while (!(ends_at >> j & 1) && (j | 1) + 1 < 2 * kSpanWaves && (valid >> ((j | 1) + 1) & 1)) {
-            j = (j | 1) + 1;
-            ++n;
-        }
-        todo &= ~((2u << j) - 1);
-        const bool whole = (starts_at >> i & 1) && (ends_at >> j & 1);
-        const int seg = __builtin_amdgcn_readlane(fr.seg, i);
-        const int sb = __builtin_amdgcn_readlane(fr.b, i), skvh = __builtin_amdgcn_readlane(fr.kvh, i);
-        const int64_t shift = aligned ? 0 : seg;  // of the workspace slots
-        const int64_t piece = u + shift;
-        for (int idx = tid; idx < group * kHeadDim; idx += kSpanThreads) {
-            const int h = idx / kHeadDim, d = idx % kHeadDim;
-            float mk[kSpanWaves], lk[kSpanWaves], ok[kSpanWaves];
-#pragma unroll
-            for (int k = 0; k < kSpanWaves; ++k) {
-                mk[k] = -INFINITY;
-                lk[k] = ok[k] = 0.f;
-                if (k < n) {
-                    const int s = k == 0 ? i & 1 : 0;
-                    mk[k] = lds.m[w + k][s][h];
-                    lk[k] = lds.l[w + k][s][h];
-                    ok[k] = reinterpret_cast<const float *>(s ? lds.buf[w + k] : lds.head[w + k])[h * OSTR + d];
-                }
-            }
-            float M = mk[0];
-#pragma unroll
-            for (int k = 1; k < kSpanWaves; ++k) M = fmaxf(M, mk[k]);
-            float lsum = 0.f, o = 0.f;
-#pragma unroll
-            for (int k = 0; k < kSpanWaves; ++k) {
-                const float wt = mk[k] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mk[k] - M);  // no keys on valid pages
-                lsum += wt * lk[k];
-                o += wt * ok[k];
-            }
-            if (whole) {
-                out[(static_cast<size_t>(sb) * hq + skvh * group + h) * kHeadDim + d] = to_bf16(o / lsum);
-            } else if (piece < slots) {
-                // device-scope stores (through the L2 of this XCD): the piece may be
-                // merged by a work-group on another XCD without a cache writeback
-                __hip_atomic_store(&ws_o[(static_cast<size_t>(piece) * group + h) * kHeadDim + d], o, __ATOMIC_RELAXED,
-                                   __HIP_MEMORY_SCOPE_AGENT);
-                if (d == 0)
-                    __hip_atomic_store(reinterpret_cast<unsigned long long *>(&ws_ml[static_cast<size_t>(piece) * group + h]),
-                                       __builtin_bit_cast(unsigned long long, make_float2(M, lsum)), __ATOMIC_RELAXED,
-                                       __HIP_MEMORY_SCOPE_AGENT);
-            }
-        }
-        if (!whole) {
-            const int64_t f0 = __builtin_amdgcn_readlane(fr.u0, i);
-            const Pending::Piece pc{sb, skvh, __builtin_amdgcn_readlane(fr.nch, i), f0 + shift, piece};
-            if (pend.n == 0)
-                pend.p0 = pc;
-            else
-                pend.p1 = pc;
-            pend.n = pend.n == 0 ? 1 : 2;
-        }
-    }
-    if (pend.n > 0)
-        finish_segments(out, ws_o, ws_ml, flags, tag, pend, slots, hkv, group, tid, lds);
+    add_up_fragments(out, ws_o, ws_ml, flags, tag, slots, hkv, group, aligned, u, tid, lds);
 }
 
 }  // namespace dk

@@ -70,7 +70,58 @@ k_kv_gather(const uint4 *__restrict__ kpool, const uint4 *__restrict__ vpool,
     }
 }
 
+// The checks and the handle that both kinds of pool share; `aligned`: the arrays are.
+mw_status create_pool(const mw_kv_pool_desc *desc, bool aligned, mw_kv_pool **out, const char *who) {
+    if (desc->num_pages < 1 || desc->num_kv_heads < 1)
+        return fail(MW_ERR_INVALID_ARG, "%s: num_pages and num_kv_heads must be >= 1", who);
+    if (desc->page_size != kPageSize || desc->head_dim != kHeadDim)
+        return fail(MW_ERR_UNSUPPORTED, "%s: only page_size 16 and head_dim 128", who);
+    if (!aligned) return fail(MW_ERR_INVALID_ARG, "%s: pool arrays must be 16-byte aligned", who);
+    mw_kv_pool *p = nullptr;
+    try {
+        p = new mw_kv_pool();
+        p->desc = *desc;
+        p->is_free.assign(desc->num_pages, 1);
+        for (int32_t i = 0; i < desc->num_pages; ++i) p->free_list.push_back(i);
+    } catch (const std::bad_alloc &) {
+        delete p;
+        return fail(MW_ERR_INVALID_ARG, "%s: out of host memory", who);
+    }
+    *out = p;
+    return MW_OK;
+}
+
 }  // namespace
+
+namespace mw {
+
+mw_status check_pool_kind(const mw_kv_pool *pool, bool four_bit, const char *who) {
+    if ((pool->k4 != nullptr) != four_bit)
+        return fail(MW_ERR_INVALID_ARG, "%s: the pool holds %s, the call is for %s", who,
+                    four_bit ? "bf16" : "4-bit codes", four_bit ? "4-bit codes" : "bf16");
+    return MW_OK;
+}
+
+mw_status check_rows(const mw_kv_pool *pool, int32_t batch, const int32_t *h_new_lens, const int32_t *h_start_pos,
+                     const int32_t *d_indptr, const int32_t *d_start_pos, const int32_t *d_block_table,
+                     int32_t bt_stride, int64_t *max_n, int64_t *total, const char *who) {
+    if (!pool || batch < 0 || (batch > 0 && (!h_new_lens || !h_start_pos || !d_indptr || !d_start_pos ||
+                                             !d_block_table)) ||
+        bt_stride < 1 || batch > 65535)
+        return fail(MW_ERR_INVALID_ARG, "%s: bad arguments", who);
+    *max_n = *total = 0;
+    for (int32_t b = 0; b < batch; ++b) {
+        const int64_t end = static_cast<int64_t>(h_start_pos[b]) + h_new_lens[b];
+        if (h_new_lens[b] < 0 || h_start_pos[b] < 0 || end > static_cast<int64_t>(bt_stride) * kPageSize)
+            return fail(MW_ERR_INVALID_ARG, "%s: sequence %d has positions [%d, %lld) beyond its table of %d pages",
+                        who, b, h_start_pos[b], static_cast<long long>(end), bt_stride);
+        *max_n = h_new_lens[b] > *max_n ? h_new_lens[b] : *max_n;
+        *total += h_new_lens[b];
+    }
+    return MW_OK;
+}
+
+}  // namespace mw
 
 extern "C" {
 
@@ -78,19 +129,26 @@ mw_status mw_kv_pool_create(const mw_kv_pool_desc *desc, void *d_k_pages, void *
                             mw_kv_pool **out) {
     if (!desc || !out || !d_k_pages || !d_v_pages)
         return fail(MW_ERR_INVALID_ARG, "mw_kv_pool_create: NULL argument");
-    if (desc->num_pages < 1 || desc->num_kv_heads < 1)
-        return fail(MW_ERR_INVALID_ARG, "mw_kv_pool_create: num_pages and num_kv_heads must be >= 1");
-    if (desc->page_size != kPageSize || desc->head_dim != kHeadDim)
-        return fail(MW_ERR_UNSUPPORTED, "mw_kv_pool_create: only page_size 16 and head_dim 128");
-    if (!aligned16(d_k_pages) || !aligned16(d_v_pages))
-        return fail(MW_ERR_INVALID_ARG, "mw_kv_pool_create: pool arrays must be 16-byte aligned");
-    mw_kv_pool *p = new (std::nothrow) mw_kv_pool();
-    if (!p) return fail(MW_ERR_INVALID_ARG, "mw_kv_pool_create: out of host memory");
-    p->desc = *desc;
+    mw_kv_pool *p = nullptr;
+    const mw_status st = create_pool(desc, aligned16(d_k_pages) && aligned16(d_v_pages), &p, "mw_kv_pool_create");
+    if (st != MW_OK) return st;
     p->k = static_cast<uint16_t *>(d_k_pages);
     p->v = static_cast<uint16_t *>(d_v_pages);
-    p->is_free.assign(desc->num_pages, 1);
-    for (int32_t i = 0; i < desc->num_pages; ++i) p->free_list.push_back(i);
+    *out = p;
+    return MW_OK;
+}
+
+mw_status mw_kv4_pool_create(const mw_kv_pool_desc *desc, void *d_k_codes, void *d_v_codes, void *d_scales,
+                             mw_kv_pool **out) {
+    if (!desc || !out || !d_k_codes || !d_v_codes || !d_scales)
+        return fail(MW_ERR_INVALID_ARG, "mw_kv4_pool_create: NULL argument");
+    mw_kv_pool *p = nullptr;
+    const mw_status st = create_pool(desc, aligned16(d_k_codes) && aligned16(d_v_codes) && aligned16(d_scales), &p,
+                                     "mw_kv4_pool_create");
+    if (st != MW_OK) return st;
+    p->k4 = static_cast<uint8_t *>(d_k_codes);
+    p->v4 = static_cast<uint8_t *>(d_v_codes);
+    p->scales = static_cast<uint8_t *>(d_scales);
     *out = p;
     return MW_OK;
 }
@@ -156,26 +214,16 @@ mw_status mw_kv_pool_write(const mw_kv_pool *pool, int32_t batch, const int32_t 
                            const int32_t *d_start_pos, const int32_t *d_block_table,
                            int32_t bt_stride, const void *d_k_new, const void *d_v_new,
                            mw_stream stream, mw_timing *timing) {
-    if (!pool || batch < 0 || (batch > 0 && (!h_new_lens || !h_start_pos || !d_qo_indptr ||
-                                             !d_start_pos || !d_block_table)) ||
-        bt_stride < 1 || batch > 65535)
-        return fail(MW_ERR_INVALID_ARG, "mw_kv_pool_write: bad arguments");
+    const char *who = "mw_kv_pool_write";
     int64_t max_n = 0, total = 0;
-    for (int32_t b = 0; b < batch; ++b) {
-        if (h_new_lens[b] < 0 || h_start_pos[b] < 0 ||
-            static_cast<int64_t>(h_start_pos[b]) + h_new_lens[b] >
-                static_cast<int64_t>(bt_stride) * kPageSize)
-            return fail(MW_ERR_INVALID_ARG,
-                        "mw_kv_pool_write: sequence %d writes positions [%d, %d) beyond its table "
-                        "of %d pages",
-                        b, h_start_pos[b], h_start_pos[b] + h_new_lens[b], bt_stride);
-        max_n = h_new_lens[b] > max_n ? h_new_lens[b] : max_n;
-        total += h_new_lens[b];
-    }
+    mw_status st = check_rows(pool, batch, h_new_lens, h_start_pos, d_qo_indptr, d_start_pos, d_block_table, bt_stride,
+                              &max_n, &total, who);
+    if (st == MW_OK) st = check_pool_kind(pool, false, who);
+    if (st != MW_OK) return st;
     if (total > 0 && (!d_k_new || !d_v_new || !aligned16(d_k_new) || !aligned16(d_v_new)))
         return fail(MW_ERR_INVALID_ARG, "mw_kv_pool_write: new K/V must be 16-byte aligned");
     hipStream_t s = static_cast<hipStream_t>(stream);
-    mw_status st = timing_begin(timing, s);
+    st = timing_begin(timing, s);
     if (st != MW_OK) return st;
     if (total > 0) {
         const int per_tok = pool->desc.num_kv_heads * kVecPerRow;
@@ -198,6 +246,8 @@ mw_status mw_kv_pool_gather(const mw_kv_pool *pool, const int32_t *d_block_table
                             void *d_k_out, void *d_v_out, mw_stream stream) {
     if (!pool || n_tokens < 0 || (n_tokens > 0 && (!d_block_table || !d_k_out || !d_v_out)))
         return fail(MW_ERR_INVALID_ARG, "mw_kv_pool_gather: bad arguments");
+    const mw_status st = check_pool_kind(pool, false, "mw_kv_pool_gather");
+    if (st != MW_OK) return st;
     if (n_tokens == 0) return MW_OK;
     if (!aligned16(d_k_out) || !aligned16(d_v_out))
         return fail(MW_ERR_INVALID_ARG, "mw_kv_pool_gather: outputs must be 16-byte aligned");

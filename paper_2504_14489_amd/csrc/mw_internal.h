@@ -85,8 +85,11 @@ int stream_cus(hipStream_t s);
 
 struct mw_kv_pool {
     mw_kv_pool_desc desc;
-    uint16_t *k;
+    uint16_t *k;      // bf16 pages; NULL in a 4-bit pool
     uint16_t *v;
+    uint8_t *k4;      // 4-bit codes and scale bytes; NULL in a bf16 pool
+    uint8_t *v4;
+    uint8_t *scales;
     std::deque<int32_t> free_list;
     std::vector<uint8_t> is_free;
 };
@@ -118,6 +121,15 @@ void timing_end(mw_timing *t);
 // Reports a failed kernel launch (bad configuration) as MW_ERR_HIP.
 mw_status check_launch(const char *what);
 
+// MW_ERR_INVALID_ARG if the pool is not of the kind (bf16, or 4 bits) that `who` reads or writes.
+mw_status check_pool_kind(const mw_kv_pool *pool, bool four_bit, const char *who);
+// The checks every append and read-back of rows makes: the arrays, the batch and
+// positions [start, start + n) of each sequence within its table.  *max_n and
+// *total: the most new rows of a sequence, and all of them.
+mw_status check_rows(const mw_kv_pool *pool, int32_t batch, const int32_t *h_new_lens, const int32_t *h_start_pos,
+                     const int32_t *d_indptr, const int32_t *d_start_pos, const int32_t *d_block_table,
+                     int32_t bt_stride, int64_t *max_n, int64_t *total, const char *who);
+
 }  // namespace mw
 
 namespace mw {
@@ -140,7 +152,11 @@ struct DecodePlan {
 // Validates a decode call's arguments (workspace size included) and plans it.
 // cus > 0 with chunk_pages = 0: the balanced split over that many CUs;
 // cus = 0: fixed chunks only (chunk_pages 0 then means automatic chunks).
-mw_status decode_prepare(const mw_decode_args *a, int64_t cus, DecodePlan *p, const char *who);
+// four_bit: the kind of pool the call reads (the other kind is refused).
+mw_status decode_prepare(const mw_decode_args *a, int64_t cus, DecodePlan *p, const char *who, bool four_bit = false);
+// A tag for the next launch of a balanced split, never 0 (the cleared flag
+// value): a done flag in a workspace counts only for the launch whose tag it shows.
+uint32_t next_decode_tag();
 // Launches the kernel that merges the chunk partials of every (sequence, kv
 // head) of a fixed-chunk split (the balanced split merges its own).
 mw_status decode_combine_launch(const mw_decode_args *a, const DecodePlan &p, hipStream_t s);
@@ -180,6 +196,9 @@ void prefill_split_plan(int32_t batch, const int32_t *h_new_lens, const int32_t 
 // what callers have always brought: prefill_base_pieces.
 mw_status prefill_fit_workspace(const mw_prefill_args *a, int64_t cus, PrefillPlan *p, const void *ws, size_t bytes,
                                 const char *who);
+// Enqueues a call that prefill_split_plan planned (its workspace is the
+// arguments'); `timing` has begun.
+mw_status prefill_launch(const mw_prefill_args &a, const PrefillPlan &pl, hipStream_t s, mw_timing *timing);
 // Pieces of a call on blocks of 32 positions x up to four query heads (1: none):
 // with fewer of them than CUs, so many that two work-groups come on a CU; with
 // fewer than two per CU, three for blocks of 96 tiles and more.  A caller that

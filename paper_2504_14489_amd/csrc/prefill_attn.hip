@@ -464,6 +464,8 @@ mw_status prefill_prepare(const mw_prefill_args *a, int64_t cus, bool allow_smal
     if (!a || !a->pool || a->batch < 0 || a->batch > 65535 || a->bt_stride < 1 ||
         (a->batch > 0 && (!a->h_new_lens || !a->h_prefix_lens)))
         return fail(MW_ERR_INVALID_ARG, "%s: bad arguments", who);
+    const mw_status kind = check_pool_kind(a->pool, false, who);
+    if (kind != MW_OK) return kind;
     const mw_attn_shape *shape = &a->shape;
     const mw_kv_pool *pool = a->pool;
     if (shape->head_dim != kHeadDim) return fail(MW_ERR_UNSUPPORTED, "%s: head_dim must be 128", who);
@@ -504,10 +506,9 @@ mw_status prefill_prepare(const mw_prefill_args *a, int64_t cus, bool allow_smal
 
 }  // namespace mw
 
-// One launch of 8- or 4-wave blocks as planned by prefill_prepare.
+// One launch of 8- or 4-wave blocks as planned by prefill_prepare; `timing` has begun.
 static mw_status launch_plain(const mw_prefill_args &a, const PrefillPlan &pl, hipStream_t s, mw_timing *timing) {
-    mw_status st = timing_begin(timing, s);
-    if (st != MW_OK) return st;
+    mw_status st = MW_OK;
     if (pl.gx > 0) {
         auto kernel = pl.waves == 4 ? (pl.table_in_lds ? k_prefill_attn<true, 4> : k_prefill_attn<false, 4>)
                                     : (pl.table_in_lds ? k_prefill_attn<true, 8> : k_prefill_attn<false, 8>);
@@ -535,6 +536,7 @@ extern "C" mw_status mw_prefill_attn(const mw_kv_pool *pool, const mw_attn_shape
     hipStream_t s = static_cast<hipStream_t>(stream);
     PrefillPlan pl;
     mw_status st = prefill_prepare(&a, stream_cus(s), true, &pl, who);
+    if (st == MW_OK) st = timing_begin(timing, s);
     if (st != MW_OK) return st;
     return launch_plain(a, pl, s, timing);
 }
@@ -559,26 +561,19 @@ extern "C" mw_status mw_prefill_workspace_size(const mw_attn_shape *shape, int32
     return MW_OK;
 }
 
-extern "C" mw_status mw_prefill_attn_ws(const mw_kv_pool *pool, const mw_attn_shape *shape, int32_t batch,
-                                        const int32_t *h_new_lens, const int32_t *h_prefix_lens,
-                                        const int32_t *d_qo_indptr, const int32_t *d_prefix_lens,
-                                        const int32_t *d_block_table, int32_t bt_stride, const void *d_q,
-                                        void *d_out, void *d_workspace, size_t workspace_bytes, mw_stream stream,
-                                        mw_timing *timing) {
-    const char *who = "mw_prefill_attn_ws";
-    if (!shape) return fail(MW_ERR_INVALID_ARG, "%s: bad arguments", who);
-    const mw_prefill_args a{pool,          *shape,        batch,     h_new_lens, h_prefix_lens, d_qo_indptr,
-                            d_prefix_lens, d_block_table, bt_stride, d_q,        d_out};
-    hipStream_t s = static_cast<hipStream_t>(stream);
-    PrefillPlan pl;
-    const int64_t cus = stream_cus(s);
-    mw_status st = prefill_prepare(&a, cus, true, &pl, who, true);
-    if (st == MW_OK) st = prefill_fit_workspace(&a, cus, &pl, d_workspace, workspace_bytes, who);
-    if (st != MW_OK) return st;
+namespace mw {
+
+mw_status prefill_launch(const mw_prefill_args &a, const PrefillPlan &pl, hipStream_t s, mw_timing *timing) {
+    const mw_kv_pool *pool = a.pool;
+    const mw_attn_shape *shape = &a.shape;
+    const int32_t batch = a.batch, bt_stride = a.bt_stride;
+    const int32_t *h_new_lens = a.h_new_lens;
+    const int32_t *d_qo_indptr = a.d_qo_indptr, *d_prefix_lens = a.d_prefix_lens, *d_block_table = a.d_block_table;
+    const void *d_q = a.d_q;
+    void *d_out = a.d_out;
+    mw_status st = MW_OK;
     if (pl.big_units > 0) {
         const int64_t n_big = pl.big_units, units = pl.gx;
-        st = timing_begin(timing, s);
-        if (st != MW_OK) return st;
         auto kernel = pl.table_in_lds ? k_prefill_mixed<true> : k_prefill_mixed<false>;
         hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(n_big + 2 * (units - n_big))), dim3(512), 0, s, pool->k,
                            pool->v, static_cast<const uint16_t *>(d_q), static_cast<uint16_t *>(d_out), d_qo_indptr,
@@ -594,10 +589,8 @@ extern "C" mw_status mw_prefill_attn_ws(const mw_kv_pool *pool, const mw_attn_sh
     const bool cut = pl.pieces > 1;
     int64_t max_n = 0;
     for (int32_t b = 0; b < batch; ++b) max_n = std::max<int64_t>(max_n, h_new_lens[b]);
-    st = timing_begin(timing, s);
-    if (st != MW_OK) return st;
-    float *ws_o = static_cast<float *>(d_workspace);
-    float2 *ws_ml = reinterpret_cast<float2 *>(static_cast<char *>(d_workspace) +
+    float *ws_o = static_cast<float *>(a.d_workspace);
+    float2 *ws_ml = reinterpret_cast<float2 *>(static_cast<char *>(a.d_workspace) +
                                                static_cast<size_t>(pl.pieces) * pl.rows * shape->num_q_heads *
                                                    kHeadDim * 4);
     auto kernel = cut ? (pl.table_in_lds ? k_prefill_dual<true, true> : k_prefill_dual<false, true>)
@@ -623,4 +616,26 @@ extern "C" mw_status mw_prefill_attn_ws(const mw_kv_pool *pool, const mw_attn_sh
     st = timing_kernel_done(timing, s);
     timing_end(timing);
     return st;
+}
+
+}  // namespace mw
+
+extern "C" mw_status mw_prefill_attn_ws(const mw_kv_pool *pool, const mw_attn_shape *shape, int32_t batch,
+                                        const int32_t *h_new_lens, const int32_t *h_prefix_lens,
+                                        const int32_t *d_qo_indptr, const int32_t *d_prefix_lens,
+                                        const int32_t *d_block_table, int32_t bt_stride, const void *d_q,
+                                        void *d_out, void *d_workspace, size_t workspace_bytes, mw_stream stream,
+                                        mw_timing *timing) {
+    const char *who = "mw_prefill_attn_ws";
+    if (!shape) return fail(MW_ERR_INVALID_ARG, "%s: bad arguments", who);
+    const mw_prefill_args a{pool,          *shape,        batch,     h_new_lens, h_prefix_lens, d_qo_indptr,
+                            d_prefix_lens, d_block_table, bt_stride, d_q,        d_out,      d_workspace,   workspace_bytes};
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    PrefillPlan pl;
+    const int64_t cus = stream_cus(s);
+    mw_status st = prefill_prepare(&a, cus, true, &pl, who, true);
+    if (st == MW_OK) st = prefill_fit_workspace(&a, cus, &pl, d_workspace, workspace_bytes, who);
+    if (st == MW_OK) st = timing_begin(timing, s);
+    if (st != MW_OK) return st;
+    return prefill_launch(a, pl, s, timing);
 }

@@ -54,6 +54,14 @@ class _AttnShape(ctypes.Structure):
                 ("head_dim", ctypes.c_int32), ("scale", ctypes.c_float)]
 
 
+class NormRope(ctypes.Structure):
+    """mw_norm_rope: what mw_qk_norm_rope_write does to queries and keys
+    (device addresses as integers, 0 for NULL)."""
+    _fields_ = [("num_q_heads", ctypes.c_int32), ("rot_dim", ctypes.c_int32), ("neighbours", ctypes.c_int32),
+                ("eps", ctypes.c_float), ("d_q_weight", ctypes.c_void_p), ("d_k_weight", ctypes.c_void_p),
+                ("d_inv_freq", ctypes.c_void_p)]
+
+
 class _DecodeArgs(ctypes.Structure):
     _fields_ = [("pool", ctypes.c_void_p), ("shape", _AttnShape), ("batch", ctypes.c_int32),
                 ("h_seq_lens", ctypes.c_void_p), ("d_seq_lens", ctypes.c_void_p),
@@ -112,6 +120,11 @@ _SIGNATURES = {
     "mw_kv_pool_num_free": ([_P, _PI], _I),
     "mw_kv_pool_write": ([_P, _I, _PI, _PI, _P, _P, _P, _I, _P, _P, _P, _P], _I),
     "mw_kv_pool_gather": ([_P, _P, _I, _P, _P, _P], _I),
+    "mw_kv4_pool_create": ([ctypes.POINTER(_PoolDesc), _P, _P, _P, ctypes.POINTER(_P)], _I),
+    "mw_kv4_pool_write": ([_P, _I, _PI, _PI, _P, _P, _P, _I, _P, _P, _P, _P], _I),
+    "mw_kv4_pool_gather": ([_P, _I, _PI, _PI, _P, _P, _P, _I, _P, _P, _P, _P], _I),
+    "mw_qk_norm_rope_write": ([_P, ctypes.POINTER(NormRope), _I, _PI, _PI, _P, _P, _P, _I, _P, ctypes.c_int64, _P,
+                               ctypes.c_int64, _P, ctypes.c_int64, _P, _P, _P], _I),
     "mw_partition_create": ([_I, _I, _I, ctypes.POINTER(_P)], _I),
     "mw_partition_create_masks": ([_I, _PU, _PU, _I, ctypes.POINTER(_P)], _I),
     "mw_partition_streams": ([_P, ctypes.POINTER(_P), ctypes.POINTER(_P)], _I),
@@ -140,6 +153,13 @@ _SIGNATURES = {
     "mw_decode_attn": ([_P, ctypes.POINTER(_AttnShape), _I, _PI, _P, _P, _I, _P, _P, _P,
                         ctypes.c_size_t, _I, _P, _P], _I),
     "mw_decode_attn_noalloc": ([_P, ctypes.POINTER(_AttnShape), _I, _PI, _P, _P, _I, _P, _P, _I, _P], _I),
+    "mw_kv4_decode_workspace_size": ([ctypes.POINTER(_AttnShape), _I, _PI, ctypes.POINTER(ctypes.c_size_t)], _I),
+    "mw_kv4_decode_attn": ([_P, ctypes.POINTER(_AttnShape), _I, _PI, _P, _P, _I, _P, _P, _P, ctypes.c_size_t, _P, _P],
+                           _I),
+    "mw_kv4_prefill_workspace_size": ([ctypes.POINTER(_AttnShape), _I, _PI, _PI, _I,
+                                       ctypes.POINTER(ctypes.c_size_t)], _I),
+    "mw_kv4_prefill_attn": ([_P, ctypes.POINTER(_AttnShape), _I, _PI, _PI, _P, _P, _P, _I, _P, _P, _P,
+                             ctypes.c_size_t, _P, _P], _I),
     "mw_predictor_create": ([ctypes.POINTER(_P)], _I),
     "mw_predictor_destroy": ([_P], _I),
     "mw_predictor_set_launch_shape": ([_P, _I, _I], _I),
@@ -291,6 +311,39 @@ def mw_kv_pool_gather(pool, d_block_table: int, n_tokens: int, d_k_out: int, d_v
                                     _h(d_v_out), _h(stream)))
 
 
+# ---------------------------------------------------- pool in 4 bits, rows ---
+def mw_kv4_pool_create(num_pages: int, page_size: int, num_kv_heads: int, head_dim: int, d_k_codes: int,
+                       d_v_codes: int, d_scales: int):
+    out = _P()
+    desc = _PoolDesc(num_pages, page_size, num_kv_heads, head_dim)
+    _check(load().mw_kv4_pool_create(ctypes.byref(desc), _h(d_k_codes), _h(d_v_codes), _h(d_scales),
+                                     ctypes.byref(out)))
+    return out
+
+
+def mw_kv4_pool_write(pool, new_lens, start_pos, d_qo_indptr: int, d_start_pos: int, d_block_table: int,
+                      bt_stride: int, d_k_new: int, d_v_new: int, stream=0, timing=None):
+    nl, sp = _i32(new_lens), _i32(start_pos)
+    _check(load().mw_kv4_pool_write(pool, len(nl), _pi(nl), _pi(sp), _h(d_qo_indptr), _h(d_start_pos),
+                                    _h(d_block_table), bt_stride, _h(d_k_new), _h(d_v_new), _h(stream), timing))
+
+
+def mw_kv4_pool_gather(pool, lens, start_pos, d_indptr: int, d_start_pos: int, d_block_table: int, bt_stride: int,
+                       d_k_out: int, d_v_out: int, stream=0, timing=None):
+    nl, sp = _i32(lens), _i32(start_pos)
+    _check(load().mw_kv4_pool_gather(pool, len(nl), _pi(nl), _pi(sp), _h(d_indptr), _h(d_start_pos),
+                                     _h(d_block_table), bt_stride, _h(d_k_out), _h(d_v_out), _h(stream), timing))
+
+
+def mw_qk_norm_rope_write(pool, rope: NormRope, new_lens, start_pos, d_qo_indptr: int, d_start_pos: int,
+                          d_block_table: int, bt_stride: int, d_q: int, q_stride: int, d_k: int, k_stride: int,
+                          d_v: int, v_stride: int, d_q_out: int, stream=0, timing=None):
+    nl, sp = _i32(new_lens), _i32(start_pos)
+    _check(load().mw_qk_norm_rope_write(pool, ctypes.byref(rope), len(nl), _pi(nl), _pi(sp), _h(d_qo_indptr),
+                                        _h(d_start_pos), _h(d_block_table), bt_stride, _h(d_q), q_stride, _h(d_k),
+                                        k_stride, _h(d_v), v_stride, _h(d_q_out), _h(stream), timing))
+
+
 # ------------------------------------------------------------- partition ---
 def mw_partition_create(device: int, prefill_cus: int, decode_cus: int):
     out = _P()
@@ -440,6 +493,44 @@ def mw_decode_attn(pool, num_q_heads: int, num_kv_heads: int, head_dim: int, sca
     _check(load().mw_decode_attn(pool, ctypes.byref(sh), len(sl), _pi(sl), _h(d_seq_lens),
                                  _h(d_block_table), bt_stride, _h(d_q), _h(d_out), _h(d_workspace),
                                  workspace_bytes, chunk_pages, _h(stream), timing))
+
+
+def mw_kv4_decode_workspace_size(num_q_heads: int, num_kv_heads: int, head_dim: int, seq_lens) -> int:
+    sl = _i32(seq_lens)
+    sh = _shape(num_q_heads, num_kv_heads, head_dim, 1.0)
+    out = ctypes.c_size_t()
+    _check(load().mw_kv4_decode_workspace_size(ctypes.byref(sh), len(sl), _pi(sl), ctypes.byref(out)))
+    return out.value
+
+
+def mw_kv4_decode_attn(pool, num_q_heads: int, num_kv_heads: int, head_dim: int, scale: float, seq_lens,
+                       d_seq_lens: int, d_block_table: int, bt_stride: int, d_q: int, d_out: int, d_workspace: int,
+                       workspace_bytes: int, stream=0, timing=None):
+    sl = _i32(seq_lens)
+    sh = _shape(num_q_heads, num_kv_heads, head_dim, scale)
+    _check(load().mw_kv4_decode_attn(pool, ctypes.byref(sh), len(sl), _pi(sl), _h(d_seq_lens), _h(d_block_table),
+                                     bt_stride, _h(d_q), _h(d_out), _h(d_workspace), workspace_bytes, _h(stream),
+                                     timing))
+
+
+def mw_kv4_prefill_workspace_size(num_q_heads: int, num_kv_heads: int, head_dim: int, new_lens, prefix_lens,
+                                  num_cus: int = 0) -> int:
+    nl, pl = _i32(new_lens), _i32(prefix_lens)
+    sh = _shape(num_q_heads, num_kv_heads, head_dim, 1.0)
+    out = ctypes.c_size_t()
+    _check(load().mw_kv4_prefill_workspace_size(ctypes.byref(sh), len(nl), _pi(nl), _pi(pl), num_cus,
+                                                ctypes.byref(out)))
+    return out.value
+
+
+def mw_kv4_prefill_attn(pool, num_q_heads: int, num_kv_heads: int, head_dim: int, scale: float, new_lens, prefix_lens,
+                        d_qo_indptr: int, d_prefix_lens: int, d_block_table: int, bt_stride: int, d_q: int,
+                        d_out: int, d_workspace: int, workspace_bytes: int, stream=0, timing=None):
+    nl, pl = _i32(new_lens), _i32(prefix_lens)
+    sh = _shape(num_q_heads, num_kv_heads, head_dim, scale)
+    _check(load().mw_kv4_prefill_attn(pool, ctypes.byref(sh), len(nl), _pi(nl), _pi(pl), _h(d_qo_indptr),
+                                      _h(d_prefix_lens), _h(d_block_table), bt_stride, _h(d_q), _h(d_out),
+                                      _h(d_workspace), workspace_bytes, _h(stream), timing))
 
 
 def mw_decode_attn_noalloc(pool, num_q_heads: int, num_kv_heads: int, head_dim: int, scale: float,

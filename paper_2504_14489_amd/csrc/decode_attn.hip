@@ -62,14 +62,25 @@ k_decode_combine(uint16_t *__restrict__ out, const int32_t *__restrict__ seq_len
 }
 
 // Balanced split: units per CU of the stream (an 8-wave work-group fills a
-// CU), and the fewest pages a unit streams (a pair per wave: short calls are
-// bound by latency, not bytes, and fewer, longer pieces leave less to merge at
-// the end).  The workspace is sized for two units per CU of a 256-CU device.
+// CU).  The workspace is sized for two units per CU of a 256-CU device.
 constexpr int64_t kBalancedPerCu = 1;
 constexpr int64_t kBalancedSizedUnits = 512;
 constexpr int64_t kBalancedMaxUnits = 256;
-constexpr int64_t kBalancedMinPages = 16;
-constexpr int64_t kBalancedMergeSteps = 3;  // a merge's time in steps of a wave
+// The split's costs on each kind of cache.
+struct SplitCost {
+    int64_t min_pages;    // the fewest pages a unit streams: a step per wave (short calls are bound by
+                          // latency, not bytes, and fewer, longer pieces leave less to merge at the end)
+    int64_t step_pages;   // of a wave
+    int64_t merge_steps;  // a merge's time in steps of a wave
+    double cu_us, all_us; // a page at a CU's own limit, and at the memory's
+};
+constexpr SplitCost kSplitBf16{16, 2, 3, 0.14, 0.00104};
+// In 4 bits: 38 batches of 1 to 256 sequences of 256 to 32768 tokens timed with
+// every split.  Units of 32 pages instead of 16 take one sequence of 8192 tokens
+// of 8 kv heads from 13.3 to 12.0 us, one of 32768 of one kv head from 18.7 to
+// 14.5; whole segments of 3 steps next to ranges of 2 take 24 of 1000 tokens from
+// 16.1 to 13.4, next to ranges of 1 one of 1500 from 11.0 to 11.5.
+constexpr SplitCost kSplitFourBit{32, 4, 1, 0.061, 0.00033};
 
 struct Plan {
     int64_t units;            // work-groups of the split kernel
@@ -98,7 +109,8 @@ void plan_layout(Plan *plan, int32_t batch, int group) {
 // automatic fixed chunks; 0 with cus > 0: the balanced split over cus CUs
 // (cus < 0: the largest balanced split, for sizing a workspace).
 mw_status plan_decode(const mw_attn_shape *shape, int32_t batch, const int32_t *h_seq_lens,
-                      int32_t chunk_pages, int32_t bt_stride, int64_t cus, Plan *plan, const char *who) {
+                      int32_t chunk_pages, int32_t bt_stride, int64_t cus, Plan *plan, const char *who,
+                      const SplitCost &cost = kSplitBf16) {
     if (!shape || batch < 0 || (batch > 0 && !h_seq_lens))
         return fail(MW_ERR_INVALID_ARG, "%s: bad arguments", who);
     if (shape->head_dim != kHeadDim) return fail(MW_ERR_UNSUPPORTED, "%s: head_dim must be 128", who);
@@ -145,7 +157,7 @@ mw_status plan_decode(const mw_attn_shape *shape, int32_t batch, const int32_t *
         const int64_t pages = count(1) * hkv, segs = static_cast<int64_t>(batch) * hkv;
         // the workspace holds two units per CU's pieces
         const auto ranges = [&](int64_t most) {
-            const int64_t n = std::max<int64_t>(1, std::min(most, (pages + kBalancedMinPages - 1) / kBalancedMinPages));
+            const int64_t n = std::max<int64_t>(1, std::min(most, (pages + cost.min_pages - 1) / cost.min_pages));
             return std::max<int64_t>(1, (pages + n - 1) / n);
         };
         const int64_t sized_range = ranges(std::min(2 * std::max<int64_t>(n_cus, 1), kBalancedSizedUnits));
@@ -166,14 +178,14 @@ mw_status plan_decode(const mw_attn_shape *shape, int32_t batch, const int32_t *
             pl->per_unit = r;
             pl->total = padded_units(r) * r;
         };
-        // a wave's pairs in a range of r pages
-        auto steps = [](int64_t r) { return ((r + 7) / 8 + 1) / 2; };
+        // a wave's steps in a range of r pages
+        auto steps = [&](int64_t r) { return ((r + 7) / 8 + cost.step_pages - 1) / cost.step_pages; };
         if (may_align && batch > 0 && segs <= most) {
-            if (steps(np_max) <= steps(pl->per_unit) + kBalancedMergeSteps) {
+            if (steps(np_max) <= steps(pl->per_unit) + cost.merge_steps) {
                 // Every segment whole in a unit of its own, if its few more
                 // steps (1.3 us each) cost no more than storing, flagging and
                 // merging its pieces (about 4 us).
-                align_to(std::max(kBalancedMinPages, np_max));
+                align_to(std::max(cost.min_pages, np_max));
             } else {
                 // Pad every segment to a multiple of the range, so that a unit
                 // holds one piece of one segment (a range that straddles two
@@ -184,7 +196,7 @@ mw_status plan_decode(const mw_attn_shape *shape, int32_t batch, const int32_t *
                 // Padding is used where the longer stream takes less than what
                 // it saves at the end: 3.4 us of second pieces' merges, or 7.5 us
                 // where whole segments leave nothing to merge.  On few CUs a CU
-                // streams at its own limit (0.14 us a page) and the range counts,
+                // streams at its own limit (bf16: 0.14 us a page) and the range counts,
                 // on many the memory's (0.00104 us a page of the call): their sum
                 // at the power 11/4, fitted to both splits of 867 batches of 1 to
                 // 252 sequences of 64 to 32768 tokens on 8 to 256 CUs, is 0.2% off
@@ -202,7 +214,7 @@ mw_status plan_decode(const mw_attn_shape *shape, int32_t batch, const int32_t *
                 }
                 const int64_t n = padded_units(lo);
                 const auto stream_us = [&](int64_t r) {
-                    return std::pow(std::pow(0.14 * r, 2.75) + std::pow(0.00104 * pages, 2.75), 1 / 2.75);
+                    return std::pow(std::pow(cost.cu_us * r, 2.75) + std::pow(cost.all_us * pages, 2.75), 1 / 2.75);
                 };
                 const double saved = lo < np_max ? 3.4 : 7.5;
                 if (n <= sized + segs - 1 && stream_us(lo) < stream_us(pl->per_unit) + saved) align_to(lo);
@@ -237,7 +249,8 @@ mw_status decode_prepare(const mw_decode_args *a, int64_t cus, DecodePlan *p, co
     if (st != MW_OK) return st;
     const mw_attn_shape *shape = &a->shape;
     Plan pl;
-    st = plan_decode(shape, a->batch, a->h_seq_lens, a->chunk_pages, a->bt_stride, cus, &pl, who);
+    st = plan_decode(shape, a->batch, a->h_seq_lens, a->chunk_pages, a->bt_stride, cus, &pl, who,
+                     four_bit ? kSplitFourBit : kSplitBf16);
     if (st != MW_OK) return st;
     if (!(shape->scale > 0.f) || !(shape->scale < INFINITY))
         return fail(MW_ERR_INVALID_ARG, "%s: scale must be positive and finite", who);

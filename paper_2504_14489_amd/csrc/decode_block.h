@@ -408,16 +408,13 @@ struct alignas(16) Fragment {
     int pad;
 };
 
-// kBuf, kHead: bytes of a wave's buffers; kHeads: most query heads of a kv head.
-template <int kBuf, int kHead, int kHeads>
-struct SpanLdsOf {
-    char buf[kSpanWaves][kBuf];    // K/V of the pair in work; at the end the wave's last fragment's O
-    char head[kSpanWaves][kHead];  // the wave's first fragment's O
-    float m[kSpanWaves][2][kHeads], l[kSpanWaves][2][kHeads];  // [first, last fragment]
+struct SpanLds {
+    char buf[kSpanWaves][kSpanBufBytes];    // K/V of the pair in work; at the end the wave's last fragment's O
+    char head[kSpanWaves][kSpanHeadBytes];  // the wave's first fragment's O
+    float m[kSpanWaves][2][16], l[kSpanWaves][2][16];  // [first, last fragment]
     Fragment frag[kSpanWaves * 2];          // [2 wave + (0: first, 1: last)]
     int done[2];                            // the pending segments' pieces are all done
 };
-using SpanLds = SpanLdsOf<kSpanBufBytes, kSpanHeadBytes, 16>;
 
 // Inclusive scan over the wave's lanes.
 __device__ inline int lane_scan(int x) {
@@ -513,11 +510,9 @@ __device__ __forceinline__ bool locate_page(Lengths &len, int hkv, int align, in
 // heads, and one head per wave of 4 with 8 pieces in flight 24 us for 43
 // pieces of 8 heads).
 constexpr int kMergeAhead = 16;
-template <class Lds>
 __device__ __forceinline__ void
 merge_segment(uint16_t *__restrict__ out, const float *__restrict__ ws_o, const float2 *__restrict__ ws_ml,
-              int64_t first, int nch, int b, int hkv, int kvh, int group, int tid, Lds &lds) {
-    static_assert(sizeof(lds.buf) >= kSpanThreads * sizeof(float2), "the shares' sums");
+              int64_t first, int nch, int b, int hkv, int kvh, int group, int tid, SpanLds &lds) {
     const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     float2 *s_acc = reinterpret_cast<float2 *>(lds.buf);  // [wave][lane]
     const int per_head = group == 1 ? 8 : group == 2 ? 4 : group <= 4 ? 2 : 1;  // waves
@@ -613,11 +608,10 @@ struct Pending {
     int n;  // pieces: 0, 1 or 2
     Piece p0, p1;
 };
-template <class Lds>
 __device__ __forceinline__ void
 finish_segments(uint16_t *__restrict__ out, const float *__restrict__ ws_o, const float2 *__restrict__ ws_ml,
                 uint32_t *__restrict__ flags, uint32_t tag, const Pending &pend, int64_t slots, int hkv, int group,
-                int tid, Lds &lds) {
+                int tid, SpanLds &lds) {
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // this wave's piece stores are complete
     __syncthreads();
     const auto in_workspace = [&](const Pending::Piece &p) {
@@ -731,11 +725,10 @@ struct SpanShare {
 // The end of a unit, after the barrier behind its waves' shares: adds up the
 // fragments that they left in LDS, writes out the segments that the unit holds
 // whole and leaves the others' sums as pieces in the workspace.
-template <class Lds>
 __device__ __forceinline__ void
 add_up_fragments(uint16_t *__restrict__ out, float *__restrict__ ws_o, float2 *__restrict__ ws_ml,
                  uint32_t *__restrict__ flags, uint32_t tag, int64_t slots, int hkv, int group, bool aligned, int u,
-                 int tid, Lds &lds) {
+                 int tid, SpanLds &lds) {
     const int lane = tid & 63, hq = hkv * group;
     // The fragments in wave order, each wave's first before its last: those of
     // one segment are neighbours.  Lane i holds record i, so finding them is

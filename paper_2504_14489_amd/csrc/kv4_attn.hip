@@ -10,6 +10,7 @@ using namespace dk;
 using namespace kv4;
 
 typedef int i32x8 __attribute__((ext_vector_type(8)));
+typedef short i16x2 __attribute__((ext_vector_type(2)));
 
 // ------------------------------------------------------------------ decode
 // The balanced split of decode_block.h (its units, shares, pieces and merge) on
@@ -31,9 +32,30 @@ typedef int i32x8 __attribute__((ext_vector_type(8)));
 //     head), with up to eight two operands hold two blocks each, with sixteen four
 //     one each; a tile's columns of other blocks are not used.
 // kHeads: 4, 8 or 16, the most query heads of a kv head.
+//
+// A unit has eight waves, with steps of four pages: sixteen with steps of two (128
+// registers, the scores' bookkeeping twice as often) took 41 us for 32 sequences
+// of 4096 tokens of 8 kv heads instead of 28, and 16.8 instead of 13 for one of 4003.
 constexpr int kStep = 4;  // pages of a wave's step
+// What the waves leave for the end of a unit: record 2 wave + i is the wave's
+// first (0) or last (1) fragment.
 template <int kHeads>
-using Span4Lds = SpanLdsOf<kHeads * OSTR * 4, kHeads * OSTR * 4, kHeads>;
+struct Span4Lds {
+    static constexpr int kRecords = 2 * kSpanWaves;
+    float o[kRecords][kHeads][OSTR];
+    float2 ml[kRecords][kHeads];
+    Fragment frag[kRecords];
+    int done[2];  // the pending segments' pieces are all done
+};
+
+// Two bf16 values into half kHalf of hi and lo.
+template <int kHalf>
+__device__ __forceinline__ void split2(uint32_t two, float unit, i16x2 &hi, i16x2 &lo) {
+    hi = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(hi, __builtin_bit_cast(bf16x2_t, two), unit, kHalf);
+    const auto near = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(__builtin_bit_cast(int, hi), unit, kHalf);
+    lo = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(lo, __builtin_bit_cast(float, two << 16) - near[0],
+                                                  __builtin_bit_cast(float, two & 0xffff0000u) - near[1], unit, kHalf);
+}
 
 // hi and lo operands of a Q row and the factor of its scores; x[i]: the lane's
 // dims 64 (i / 2) + 16 g + 8 (i % 2) .. +7 of its column's row.
@@ -46,29 +68,198 @@ __device__ __forceinline__ float split_q(const uint4 (&x)[4], i32x8 &hi, i32x8 &
     most = max(most, static_cast<uint32_t>(__shfl_xor(static_cast<int>(most), 32)));
     const int power = static_cast<int>(most >> 7);
     const int e = max(power - 127 - 7, -100);  // rows below 2^-93 keep fewer bits
-    const float down = __builtin_bit_cast(float, static_cast<uint32_t>(127 - e) << 23);
+    const float unit = __builtin_bit_cast(float, static_cast<uint32_t>(127 + e) << 23);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-            float f[4];
-#pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                f[2 * k] = __builtin_bit_cast(float, w[2 * j + k] << 16) * down;
-                f[2 * k + 1] = __builtin_bit_cast(float, w[2 * j + k] & 0xffff0000u) * down;
-            }
-            int h = __builtin_amdgcn_cvt_pk_fp8_f32(f[0], f[1], 0, false);
-            h = __builtin_amdgcn_cvt_pk_fp8_f32(f[2], f[3], h, true);
-            const auto a = __builtin_amdgcn_cvt_pk_f32_fp8(h, false), b = __builtin_amdgcn_cvt_pk_f32_fp8(h, true);
-            int l = __builtin_amdgcn_cvt_pk_fp8_f32(f[0] - a[0], f[1] - a[1], 0, false);
-            l = __builtin_amdgcn_cvt_pk_fp8_f32(f[2] - b[0], f[3] - b[1], l, true);
-            hi[2 * i + j] = h;
-            lo[2 * i + j] = l;
+            i16x2 h{0, 0}, l{0, 0};
+            split2<0>(w[2 * j], unit, h, l);
+            split2<1>(w[2 * j + 1], unit, h, l);
+            hi[2 * i + j] = __builtin_bit_cast(int, h);
+            lo[2 * i + j] = __builtin_bit_cast(int, l);
         }
     }
     // a row that is not finite: NaN scores
-    return power == 255 ? NAN : __builtin_bit_cast(float, static_cast<uint32_t>(127 + e) << 23);
+    return power == 255 ? NAN : unit;
+}
+
+// Weighted sum of the fragments or pieces of one head in a wave: (m, l) of up to
+// 64 of them one per lane, which gives every weight 2^(m - M) and the denominator
+// within the wave, then two outputs per lane.  Those without keys have l = 0 and
+// contribute nothing.  load_o(j): the lane's two values of the j-th, j < n.
+struct HeadSum {
+    float M = -INFINITY, L = 0.f;
+    float2 acc = make_float2(0.f, 0.f);
+    template <class LoadO>
+    __device__ __forceinline__ void add(float2 ml, int n, int lane, const LoadO &load_o) {
+        const bool in = lane < n && ml.y != 0.f;
+        const float top = fmaxf(M, wave_max(in ? ml.x : -INFINITY));
+        const float old = L == 0.f ? 0.f : __builtin_amdgcn_exp2f(M - top);
+        const float w = in ? __builtin_amdgcn_exp2f(ml.x - top) : 0.f;
+        M = top;
+        L = L * old + wave_sum(in ? w * ml.y : 0.f);
+        acc.x *= old;
+        acc.y *= old;
+#pragma unroll 1
+        for (int j0 = 0; j0 < n; j0 += 8) {
+            float2 o[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) o[k] = load_o(min(j0 + k, n - 1));
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                // lanes from n on have weight 0, and j0 + k < 64
+                const float wk = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, w), j0 + k));
+                acc.x += wk * o[k].x;
+                acc.y += wk * o[k].y;
+            }
+        }
+    }
+};
+
+// The end of a unit, after the barrier behind its waves' shares: as
+// add_up_fragments and finish_segments of the bf16 cache (the same pieces, slots
+// and flags), a head at a time per wave, the heads of several runs of fragments,
+// and of both segments that are merged, side by side.
+template <int kHeads>
+__device__ __forceinline__ void
+finish_unit(uint16_t *__restrict__ out, float *__restrict__ ws_o, float2 *__restrict__ ws_ml,
+            uint32_t *__restrict__ flags, uint32_t tag, int64_t slots, int hkv, int group, bool aligned, int u, int tid,
+            Span4Lds<kHeads> &lds) {
+    constexpr int kRecords = Span4Lds<kHeads>::kRecords;
+    const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const auto write = [&](int b, int kvh, int h, const HeadSum &s) __attribute__((always_inline)) {
+        const float inv = 1.f / s.L;
+        reinterpret_cast<uint32_t *>(out + (static_cast<size_t>(b) * hkv * group + kvh * group + h) * kHeadDim)[lane] =
+            cvt2(s.acc.x * inv, s.acc.y * inv);
+    };
+    const Fragment fr = lds.frag[lane & (kRecords - 1)];
+    const bool mine = lane < kRecords && fr.seg >= 0;
+    uint32_t todo = static_cast<uint32_t>(__builtin_amdgcn_ballot_w64(mine));
+    const uint32_t valid = todo, starts_at = static_cast<uint32_t>(__builtin_amdgcn_ballot_w64(mine && fr.starts)),
+                   ends_at = static_cast<uint32_t>(__builtin_amdgcn_ballot_w64(mine && fr.ends));
+    Pending pend{};
+    int turn = wave;  // the wave's head of the next run
+#pragma unroll 1
+    while (todo) {
+        // the run: record i and the first fragments of the waves after it
+        const int i = __builtin_ctz(todo), w = i >> 1;
+        int j = i, n = 1;
+        while (!(ends_at >> j & 1) && (j | 1) + 1 < kRecords && (valid >> ((j | 1) + 1) & 1)) {
+            j = (j | 1) + 1;
+            ++n;
+        }
+        todo &= ~((2u << j) - 1);
+        const bool whole = (starts_at >> i & 1) && (ends_at >> j & 1);
+        const int sb = __builtin_amdgcn_readlane(fr.b, i), skvh = __builtin_amdgcn_readlane(fr.kvh, i);
+        const int64_t shift = aligned ? 0 : __builtin_amdgcn_readlane(fr.seg, i);  // of the workspace slots
+        const int64_t piece = u + shift;
+#pragma unroll 1
+        for (int h = turn & (kSpanWaves - 1); h < group; h += kSpanWaves) {
+            HeadSum s;
+            const float2 ml = lds.ml[lane == 0 ? i : min(2 * (w + lane), kRecords - 1)][h];
+            s.add(ml, n, lane, [&](int k) __attribute__((always_inline)) {
+                return reinterpret_cast<const float2 *>(lds.o[k == 0 ? i : 2 * (w + k)][h])[lane];
+            });
+            if (whole) {
+                write(sb, skvh, h, s);
+            } else if (piece < slots) {
+                // device-scope stores (through the L2 of this XCD): the piece may be
+                // merged by a work-group on another XCD without a cache writeback
+                const size_t at = static_cast<size_t>(piece) * group + h;
+                __hip_atomic_store(reinterpret_cast<unsigned long long *>(ws_o + at * kHeadDim) + lane,
+                                   __builtin_bit_cast(unsigned long long, s.acc), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                if (lane == 0)
+                    __hip_atomic_store(reinterpret_cast<unsigned long long *>(ws_ml + at),
+                                       __builtin_bit_cast(unsigned long long, make_float2(s.M, s.L)), __ATOMIC_RELAXED,
+                                       __HIP_MEMORY_SCOPE_AGENT);
+            }
+        }
+        turn += kSpanWaves - (group & (kSpanWaves - 1));
+        if (!whole) {
+            const Pending::Piece pc{sb, skvh, __builtin_amdgcn_readlane(fr.nch, i), __builtin_amdgcn_readlane(fr.u0, i) + shift, piece};
+            if (pend.n == 0)
+                pend.p0 = pc;
+            else
+                pend.p1 = pc;
+            pend.n = pend.n == 0 ? 1 : 2;
+        }
+    }
+    if (pend.n == 0) return;
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // this wave's piece stores are complete
+    __syncthreads();
+    // device lengths that disagree with the host's must not lead outside the
+    // workspace
+    const auto in_workspace = [&](const Pending::Piece &p) {
+        return p.first >= 0 && p.first + p.nch - 1 < slots && p.self < slots;
+    };
+    const bool ok0 = in_workspace(pend.p0), ok1 = pend.n > 1 && in_workspace(pend.p1);
+    if (tid == 0) {
+        if (ok0) __hip_atomic_store(flags + pend.p0.self, tag, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        if (ok1) __hip_atomic_store(flags + pend.p1.self, tag, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        lds.done[0] = ok0;
+        lds.done[1] = ok1;
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    }
+    __syncthreads();
+    // both segments' flags in one round of loads, half of the waves each
+    const int second = wave / (kSpanWaves / 2);
+    if (second ? ok1 : ok0) {
+        const Pending::Piece &p = second ? pend.p1 : pend.p0;
+        bool all = true;
+        for (int j = tid & (kSpanThreads / 2 - 1); j < p.nch; j += kSpanThreads / 2)
+            all = all && __hip_atomic_load(flags + p.first + j, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == tag;
+        if (!all) lds.done[second] = 0;
+    }
+    __syncthreads();
+    // the heads of what is done, over the waves
+    const int n0 = __builtin_amdgcn_readfirstlane(lds.done[0]) ? group : 0;
+    const int n1 = __builtin_amdgcn_readfirstlane(lds.done[1]) ? group : 0;
+#pragma unroll 1
+    for (int t = wave; t < n0 + n1; t += kSpanWaves) {
+        const Pending::Piece p = t < n0 ? pend.p0 : pend.p1;
+        const int h = t < n0 ? t : t - n0;
+        HeadSum s;
+        const unsigned long long *ml_src = reinterpret_cast<const unsigned long long *>(ws_ml) + p.first * group + h;
+        const unsigned long long *o_src =
+            reinterpret_cast<const unsigned long long *>(ws_o) + (p.first * group + h) * (kHeadDim / 2) + lane;
+        const int step = group * (kHeadDim / 2);
+#pragma unroll 1
+        for (int jb = 0; jb < p.nch; jb += 64) {
+            const int n = min(p.nch - jb, 64);
+            const float2 ml = __builtin_bit_cast(
+                float2, __hip_atomic_load(ml_src + (jb + min(lane, n - 1)) * group, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
+            s.add(ml, n, lane, [&](int k) __attribute__((always_inline)) {
+                return __builtin_bit_cast(float2, __hip_atomic_load(o_src + static_cast<int64_t>(jb + k) * step, __ATOMIC_RELAXED,
+                                                                    __HIP_MEMORY_SCOPE_AGENT));
+            });
+        }
+        write(p.b, p.kvh, h, s);
+        // a merged segment's flags are cleared, for a replay of this launch
+        if (h == 0)
+            for (int j = lane; j < p.nch; j += 64)
+                __hip_atomic_store(flags + p.first + j, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
+}
+
+// The larger of m and four scores; a NaN wins, which spares the instructions that
+// would quiet it (its column comes out as NaN).
+__device__ __forceinline__ float max4(float m, f32x4 s) {
+    return __builtin_elementwise_maximum(
+        __builtin_elementwise_maximum(__builtin_elementwise_maximum(m, s[0]), s[1]),
+        __builtin_elementwise_maximum(s[2], s[3]));
+}
+// x of the four lanes of a column (those 16 and 32 apart) combined by f, in each.
+template <class F>
+__device__ __forceinline__ float across(float x, const F &f) {
+    const auto pair = [&](auto r) {
+        const uint32_t lo = r[0], hi = r[1];  // (a bit cast of an element itself takes the first one)
+        return f(__builtin_bit_cast(float, lo), __builtin_bit_cast(float, hi));
+    };
+    const uint32_t a = __builtin_bit_cast(uint32_t, x);
+    const uint32_t b = __builtin_bit_cast(uint32_t, pair(__builtin_amdgcn_permlane16_swap(a, a, false, false)));
+    return pair(__builtin_amdgcn_permlane32_swap(b, b, false, false));
 }
 
 __device__ __forceinline__ bf16x8 v_operand(uint4 a, uint4 b, int t) {
@@ -100,13 +291,16 @@ k_kv4_decode(const uint8_t *__restrict__ kpool, const uint8_t *__restrict__ vpoo
 
     i32x8 q_hi, q_lo;
     float q_scale = 0.f;
+    uint4 q_next[4];  // the next fragment's rows, on their way since its chunk is known
     auto load_q = [&](const Chunk &c) __attribute__((always_inline)) {
         const uint16_t *qp = q + (static_cast<size_t>(c.b) * hq + c.kvh * group + (in_group ? head : 0)) * kHeadDim + 16 * grp;
-        uint4 x[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            x[i] = sel4(in_group, *reinterpret_cast<const uint4 *>(qp + 64 * (i >> 1) + 8 * (i & 1)));
-        q_scale = split_q(x, q_hi, q_lo) * scale_log2;
+        for (int i = 0; i < 4; ++i) q_next[i] = *reinterpret_cast<const uint4 *>(qp + 64 * (i >> 1) + 8 * (i & 1));
+    };
+    auto take_q = [&]() __attribute__((always_inline)) {
+        // (above 0, or a masked score would be a NaN; of a NaN row, NaN)
+        const float f = split_q(q_next, q_hi, q_lo) * scale_log2;
+        q_scale = f < 1e-37f ? 1e-37f : f;
     };
 
     // a step's pages: K codes of key lane%16, block lane/16, and that scale byte;
@@ -141,12 +335,12 @@ k_kv4_decode(const uint8_t *__restrict__ kpool, const uint8_t *__restrict__ vpoo
                 ks[j] = scales[static_cast<size_t>(at[j]) * kScaleBytes + lane];
             }
     };
-    auto load_v = [&](const uint32_t (&from)[kStep], int ok) __attribute__((always_inline)) {
+    auto load_v = [&]() __attribute__((always_inline)) {
 #pragma unroll
         for (int j = 0; j < kStep; ++j)
-            if (ok >> j & 1) {
-                vr[j] = load_stream(reinterpret_cast<const uint16_t *>(vpool + static_cast<size_t>(from[j]) * kCodeBytes + lane * 16));
-                const uint8_t *sc = scales + static_cast<size_t>(from[j]) * kScaleBytes + kBlocks * kPageSize + 4 * grp;
+            if (step_ok >> j & 1) {
+                vr[j] = load_stream(reinterpret_cast<const uint16_t *>(vpool + static_cast<size_t>(at[j]) * kCodeBytes + lane * 16));
+                const uint8_t *sc = scales + static_cast<size_t>(at[j]) * kScaleBytes + kBlocks * kPageSize + 4 * grp;
 #pragma unroll
                 for (int o = 0; o < kOps; ++o)
                     vs[j][o] = *reinterpret_cast<const uint32_t *>(sc + (o * kPerOp + side) * kPageSize);
@@ -185,9 +379,12 @@ k_kv4_decode(const uint8_t *__restrict__ kpool, const uint8_t *__restrict__ vpoo
         int tbl_n = nxt.valid ? walk.table(nxt) : 0;
         step_pages(cur, tbl, cur.p);
         load_k();
-        load_v(at, step_ok);
+        load_v();
+        take_q();
         for (;;) {
             const bool frag_end = !nxt.valid || nxt.b != cur.b || nxt.kvh != cur.kvh;
+            // its queries are on their way since the next fragment's chunk is known
+            if (frag_end && nxt.valid) load_q(nxt);
             for (int p = cur.p; p < cur.p_end; p += kStep) {
                 const int ok = step_ok;
                 // a step with a missing page, or past the sequence's end
@@ -202,24 +399,14 @@ k_kv4_decode(const uint8_t *__restrict__ kpool, const uint8_t *__restrict__ vpoo
                     sc[j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, q_hi, f32x4{0.f, 0.f, 0.f, 0.f}, 4, 0, 0, s, 0, 127);
                     sc[j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, q_lo, sc[j], 4, 0, 0, s, 0, 127);
                 }
-                const float q_now = q_scale;
                 // the next step's K loads go out while this one is computed, its V
                 // loads once this one's V is used
                 const bool last = p + kStep >= cur.p_end;
                 const bool more = !last || nxt.valid;
                 if (more) {
-                    if (last)
-                        step_pages(nxt, tbl_n, nxt.p);
-                    else
-                        step_pages(cur, tbl, p + kStep);
+                    step_pages(last ? nxt : cur, last ? tbl_n : tbl, last ? nxt.p : p + kStep);
                     load_k();
                 }
-                if (last && frag_end && nxt.valid) load_q(nxt);
-                float mx = -INFINITY;
-#pragma unroll
-                for (int j = 0; j < kStep; ++j)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) sc[j][i] *= q_now;
                 if (edge) {
                     // scores of keys on an absent page or past the sequence's end are
                     // masked, and their V scales are zeros (a masked key has p = 0,
@@ -234,10 +421,10 @@ k_kv4_decode(const uint8_t *__restrict__ kpool, const uint8_t *__restrict__ vpoo
                         for (int o = 0; o < kOps; ++o) vs[j][o] &= mask;
                     }
                 }
+                float mx = -INFINITY;
 #pragma unroll
-                for (int j = 0; j < kStep; ++j) mx = fmaxf(mx, fmaxf(fmaxf(sc[j][0], sc[j][1]), fmaxf(sc[j][2], sc[j][3])));
-                mx = fmaxf(mx, __shfl_xor(mx, 16));
-                mx = fmaxf(mx, __shfl_xor(mx, 32));
+                for (int j = 0; j < kStep; ++j) mx = max4(mx, sc[j]);
+                mx = across(mx, [](float a, float b) { return __builtin_elementwise_maximum(a, b); }) * q_scale;
                 if (__builtin_amdgcn_ballot_w64(mx > m_run + kRescaleLog2) != 0) {
                     const float m_new = fmaxf(m_run, mx);
                     const float alpha = __builtin_amdgcn_exp2f(m_run - m_new);
@@ -247,12 +434,11 @@ k_kv4_decode(const uint8_t *__restrict__ kpool, const uint8_t *__restrict__ vpoo
                     for (int t = 0; t < 8; ++t) oacc[t] *= alpha;
                 }
 #pragma unroll
-                for (int j = 0; j < kStep; ++j)
+                for (int j = 0; j < kStep; ++j) {
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        sc[j][i] = __builtin_amdgcn_exp2f(sc[j][i] - m_run);
-                        l_run += sc[j][i];
-                    }
+                    for (int i = 0; i < 4; ++i) sc[j][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[j][i], q_scale, -m_run));
+                    l_run += (sc[j][0] + sc[j][1]) + (sc[j][2] + sc[j][3]);
+                }
                 // P^T operands of two pages: k-slot e < 4 is token 4grp + e of the
                 // first, e >= 4 token 4grp + e - 4 of the second, as in V's layout.
                 // bf16, as in the bf16 cache's kernels (a scale is a power of two, so
@@ -271,48 +457,41 @@ k_kv4_decode(const uint8_t *__restrict__ kpool, const uint8_t *__restrict__ vpoo
                         for (int t = 2 * o * kPerOp; t < 2 * (o + 1) * kPerOp; ++t)
                             oacc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v_operand(vr[j], vr[j + 1], t), pop, oacc[t], 0, 0, 0);
                     }
-                if (more) load_v(at, step_ok);
+                if (more) load_v();
             }
             if (frag_end) {
-                l_run += __shfl_xor(l_run, 16);
-                l_run += __shfl_xor(l_run, 32);
+                l_run = across(l_run, [](float a, float b) { return a + b; });
                 const bool starts = frag_p == 0, ends = cur.p_end == cur.np;
-                if (starts && ends) {
-                    const float inv = 1.f / l_run;
-                    uint16_t *orow = out + (static_cast<size_t>(cur.b) * hq + cur.kvh * group + head) * kHeadDim + 32 * side + 8 * grp;
+                const bool whole = starts && ends;
+                // only the share's first fragment continues an earlier page
+                const int rec = 2 * wave + (starts ? 1 : 0);
+                const float inv = 1.f / l_run;
+                uint16_t *orow = out + (static_cast<size_t>(cur.b) * hq + cur.kvh * group + head) * kHeadDim + 32 * side + 8 * grp;
+                float *so = &lds.o[rec][head][32 * side + 8 * grp];
 #pragma unroll
-                    for (int o = 0; o < kOps; ++o) {
-                        float x[8];
-                        outputs(o, x);
-                        if (in_group)
+                for (int o = 0; o < kOps; ++o) {
+                    float x[8];
+                    outputs(o, x);
+                    if (in_group) {
+                        if (whole) {
                             *reinterpret_cast<uint4 *>(orow + 32 * o * kPerOp) =
                                 make_uint4(cvt2(x[0] * inv, x[1] * inv), cvt2(x[2] * inv, x[3] * inv),
                                            cvt2(x[4] * inv, x[5] * inv), cvt2(x[6] * inv, x[7] * inv));
-                    }
-                } else {
-                    // only the share's first fragment continues an earlier page
-                    const int slot = starts ? 1 : 0;
-                    float *so = reinterpret_cast<float *>(starts ? lds.buf[wave] : lds.head[wave]) + head * OSTR + 32 * side + 8 * grp;
-#pragma unroll
-                    for (int o = 0; o < kOps; ++o) {
-                        float x[8];
-                        outputs(o, x);
-                        if (in_group) {
+                        } else {
                             *reinterpret_cast<f32x4 *>(so + 32 * o * kPerOp) = f32x4{x[0], x[1], x[2], x[3]};
                             *reinterpret_cast<f32x4 *>(so + 32 * o * kPerOp + 4) = f32x4{x[4], x[5], x[6], x[7]};
                         }
                     }
-                    if (grp == 0 && side == 0) {
-                        lds.m[wave][slot][head] = m_run;
-                        lds.l[wave][slot][head] = l_run;
-                    }
+                }
+                if (!whole) {
+                    if (grp == 0 && side == 0) lds.ml[rec][head] = make_float2(m_run, l_run);
                     const int extent = aligned ? (cur.np + align - 1) / align * align : cur.np;
                     const int f0 = cur.first / per_unit, f1 = (cur.first + extent - 1) / per_unit;
                     if (lane == 0)
-                        lds.frag[2 * wave + slot] =
-                            Fragment{cur.b * hkv + cur.kvh, cur.b, cur.kvh, starts, ends, f0, f1 - f0 + 1, 0};
+                        lds.frag[rec] = Fragment{cur.b * hkv + cur.kvh, cur.b, cur.kvh, starts, ends, f0, f1 - f0 + 1, 0};
                 }
                 if (!nxt.valid) break;
+                take_q();
                 reset();
                 frag_p = nxt.p;
             }
@@ -323,7 +502,7 @@ k_kv4_decode(const uint8_t *__restrict__ kpool, const uint8_t *__restrict__ vpoo
         }
     }
     __syncthreads();
-    add_up_fragments(out, ws_o, ws_ml, flags, tag, slots, hkv, group, aligned, u, tid, lds);
+    finish_unit<kHeads>(out, ws_o, ws_ml, flags, tag, slots, hkv, group, aligned, u, tid, lds);
 }
 
 // ----------------------------------------------------------------- prefill

@@ -108,40 +108,27 @@ __device__ __forceinline__ uint32_t by_dim(uint32_t tokens) {
     return gather(tokens & 0x0f0f0f0fu) | gather(tokens >> 4 & 0x0f0f0f0fu) << 16;
 }
 
-// V of four consecutive tokens of a page: x[k][b] has dims 32b + 2c, + 1 of
-// token k.  codes[b]: the lane's four bytes of block b; bytes[b]: the scale
-// bytes of the four tokens, in every lane of the 16.
-__device__ __forceinline__ void encode_v(const uint32_t (&x)[4][kBlocks], uint32_t (&codes)[kBlocks],
+// V of token k of a quad: x[b] has dims 32b + 2c, + 1.  Adds its codes (by token)
+// and scale bytes, which every lane of the 16 gets, to those of the blocks.
+__device__ __forceinline__ void encode_v(const uint32_t (&x)[kBlocks], int k, uint32_t (&codes)[kBlocks],
                                          uint32_t (&bytes)[kBlocks]) {
+    // magnitudes of blocks 0, 1 and of blocks 2, 3 side by side, over the 16 lanes
+    uint32_t most[2];
 #pragma unroll
-    for (int b = 0; b < kBlocks; ++b) codes[b] = bytes[b] = 0;
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        // magnitudes of blocks 0, 1 and of blocks 2, 3 side by side, over the 16 lanes
-        uint32_t most[2];
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const uint32_t lo = abs2(x[k][2 * i]), hi = abs2(x[k][2 * i + 1]);
-            uint32_t m = max2((lo & 0xffff) | hi << 16, lo >> 16 | (hi & 0xffff0000u));
-            m = max2(m, dpp<kXor1>(m));
-            m = max2(m, dpp<kXor2>(m));
-            m = max2(m, dpp<kHalfMirror>(m));
-            most[i] = max2(m, dpp<kMirror>(m));
-        }
-#pragma unroll
-        for (int b = 0; b < kBlocks; ++b) {
-            const uint32_t byte = scale_byte(b & 1 ? most[b >> 1] >> 16 : most[b >> 1] & 0xffff);
-            const float scale = encode_scale(byte);
-            bytes[b] |= byte << (8 * k);
-            const uint32_t v = byte == 255 ? 0 : x[k][b];
-            codes[b] = k == 0 ? encode2<0>(codes[b], v, scale)
-                       : k == 1 ? encode2<1>(codes[b], v, scale)
-                       : k == 2 ? encode2<2>(codes[b], v, scale)
-                                : encode2<3>(codes[b], v, scale);
-        }
+    for (int i = 0; i < 2; ++i) {
+        const uint32_t lo = abs2(x[2 * i]), hi = abs2(x[2 * i + 1]);
+        uint32_t m = max2((lo & 0xffff) | hi << 16, lo >> 16 | (hi & 0xffff0000u));
+        m = max2(m, dpp<kXor1>(m));
+        m = max2(m, dpp<kXor2>(m));
+        m = max2(m, dpp<kHalfMirror>(m));
+        most[i] = max2(m, dpp<kMirror>(m));
     }
 #pragma unroll
-    for (int b = 0; b < kBlocks; ++b) codes[b] = by_dim(codes[b]);
+    for (int b = 0; b < kBlocks; ++b) {
+        const uint32_t byte = scale_byte(b & 1 ? most[b >> 1] >> 16 : most[b >> 1] & 0xffff);
+        bytes[b] |= byte << (8 * k);
+        codes[b] |= byte == 255 ? 0 : encode2<0>(0, x[b], scale_of(byte)) << (8 * k);
+    }
 }
 
 // The inverse: x[k][b] from the codes of block b, kept by dim, and its tokens' scale bytes.
@@ -161,27 +148,44 @@ __device__ __forceinline__ uint4 decode_k(uint32_t codes, uint32_t byte) {
     return make_uint4(decode2<0>(codes, scale), decode2<1>(codes, scale), decode2<2>(codes, scale), decode2<3>(codes, scale));
 }
 
-// Stores V of tokens [t0, t1) of quad g of a (page, kv head) from a lane of the
-// 16: whole bytes, those of the other tokens of the quad as they were.
-__device__ __forceinline__ void store_v(uint8_t *__restrict__ codes_at, uint8_t *__restrict__ scales_at,
-                                        const uint32_t (&codes)[kBlocks], const uint32_t (&bytes)[kBlocks], int g, int t0,
-                                        int t1, int c) {
+// Quantises and stores V of tokens [t0, t1) of quad g of a (page, kv head), token
+// t's row at src + t stride, with 16 lanes: whole bytes, those of the quad's other
+// tokens as they were.
+__device__ __forceinline__ void write_v(const uint16_t *__restrict__ src, int64_t stride, uint8_t *__restrict__ codes_at,
+                                        uint8_t *__restrict__ scales_at, int g, int t0, int t1, int c) {
     uint4 *dst = reinterpret_cast<uint4 *>(codes_at + g * 256 + c * 16);
-    uint8_t *sc = scales_at + kBlocks * kPageSize + 4 * g;
-    uint4 out = make_uint4(codes[0], codes[1], codes[2], codes[3]);
-    const uint32_t mine = c == 0 ? bytes[0] : c == 1 ? bytes[1] : c == 2 ? bytes[2] : bytes[3];
-    if (t0 == 0 && t1 == 4) {
-        if (c < kBlocks) *reinterpret_cast<uint32_t *>(sc + c * kPageSize) = mine;
-    } else {
-        const uint32_t half = (1u << 4 * t1) - (1u << 4 * t0);  // the tokens' codes of one dim
-        const uint32_t mask = half | half << 16;
-        const uint4 old = *dst;
-        out = make_uint4((out.x & mask) | (old.x & ~mask), (out.y & mask) | (old.y & ~mask),
-                         (out.z & mask) | (old.z & ~mask), (out.w & mask) | (old.w & ~mask));
-        if (c < kBlocks)
-            for (int t = t0; t < t1; ++t) sc[c * kPageSize + t] = static_cast<uint8_t>(mine >> (8 * t));
+    uint8_t *sc = scales_at + (kBlocks + (c & 3)) * kPageSize + 4 * g;  // lanes 0..3
+    const auto load = [&](int t, uint32_t (&x)[kBlocks]) __attribute__((always_inline)) {
+#pragma unroll
+        for (int k = 0; k < kBlocks; ++k) x[k] = *reinterpret_cast<const uint32_t *>(src + t * stride + 32 * k + 2 * c);
+    };
+    uint32_t codes[kBlocks] = {0, 0, 0, 0}, bytes[kBlocks] = {0, 0, 0, 0};
+    if (t1 - t0 == 4) {
+        uint32_t x[4][kBlocks];
+#pragma unroll
+        for (int t = 0; t < 4; ++t) load(t, x[t]);
+#pragma unroll
+        for (int t = 0; t < 4; ++t) encode_v(x[t], t, codes, bytes);
+        *dst = make_uint4(by_dim(codes[0]), by_dim(codes[1]), by_dim(codes[2]), by_dim(codes[3]));
+        if (c < kBlocks) *reinterpret_cast<uint32_t *>(sc) = c == 0 ? bytes[0] : c == 1 ? bytes[1] : c == 2 ? bytes[2] : bytes[3];
+        return;
     }
-    *dst = out;
+    // a single token of a decode step, or a chunk's first or last ones
+    const uint4 old = *dst;
+#pragma unroll 1
+    for (int t = t0; t < t1; ++t) {
+        uint32_t x[kBlocks];
+        load(t, x);
+        encode_v(x, t, codes, bytes);
+    }
+    const uint32_t half = (1u << 4 * t1) - (1u << 4 * t0);  // the tokens' codes of one dim
+    const uint32_t mask = half | half << 16;
+    *dst = make_uint4((by_dim(codes[0]) & mask) | (old.x & ~mask), (by_dim(codes[1]) & mask) | (old.y & ~mask),
+                      (by_dim(codes[2]) & mask) | (old.z & ~mask), (by_dim(codes[3]) & mask) | (old.w & ~mask));
+    if (c < kBlocks) {
+        const uint32_t mine = c == 0 ? bytes[0] : c == 1 ? bytes[1] : c == 2 ? bytes[2] : bytes[3];
+        for (int t = t0; t < t1; ++t) sc[t] = static_cast<uint8_t>(mine >> (8 * t));
+    }
 }
 
 }  // namespace kv4

@@ -30,6 +30,33 @@ __device__ __forceinline__ bool find_quad(Quad &q, int quad, int pos0, int n, co
     return q.page >= 0 && q.page < num_pages;
 }
 
+// K of tokens [t0, t1) of quad g, token t's row at src + t stride.
+__device__ __forceinline__ void write_k(const uint16_t *__restrict__ src, int64_t stride, uint8_t *__restrict__ codes_at,
+                                        uint8_t *__restrict__ scales_at, int g, int t0, int t1, int c) {
+    uint32_t *dst = reinterpret_cast<uint32_t *>(codes_at + 4 * g * (kHeadDim / 2) + 4 * c);
+    uint8_t *sc = scales_at + (c >> 2) * kPageSize + 4 * g;
+    if (t1 - t0 == 4) {
+        uint4 x[4];
+#pragma unroll
+        for (int t = 0; t < 4; ++t) x[t] = *reinterpret_cast<const uint4 *>(src + t * stride + 8 * c);
+        uint32_t bytes = 0;
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+            uint32_t byte;
+            dst[t * (kHeadDim / 8)] = encode_k(x[t], &byte);
+            bytes |= byte << (8 * t);
+        }
+        if ((c & 3) == 0) *reinterpret_cast<uint32_t *>(sc) = bytes;
+        return;
+    }
+#pragma unroll 1
+    for (int t = t0; t < t1; ++t) {
+        uint32_t byte;
+        dst[t * (kHeadDim / 8)] = encode_k(*reinterpret_cast<const uint4 *>(src + t * stride + 8 * c), &byte);
+        if ((c & 3) == 0) sc[t] = static_cast<uint8_t>(byte);
+    }
+}
+
 __global__ void __launch_bounds__(256)
 k_kv4_write(uint8_t *__restrict__ kpool, uint8_t *__restrict__ vpool, uint8_t *__restrict__ scales,
             const uint16_t *__restrict__ knew, const uint16_t *__restrict__ vnew, const int32_t *__restrict__ indptr,
@@ -46,30 +73,11 @@ k_kv4_write(uint8_t *__restrict__ kpool, uint8_t *__restrict__ vpool, uint8_t *_
         const int h = static_cast<int>(static_cast<uint32_t>(idx) - static_cast<uint32_t>(i) * hkv);
         Quad q;
         if (!find_quad(q, quad0 + i, pos0, n, btrow, bt_stride, num_pages)) continue;
-        uint4 kr[4];
-        uint32_t vr[4][kBlocks];
-#pragma unroll
-        for (int t = 0; t < 4; ++t) {
-            const bool in = t >= q.t0 && t < q.t1;
-            const size_t src = (static_cast<size_t>(row0 + q.row + t) * hkv + h) * kHeadDim;
-            kr[t] = in ? *reinterpret_cast<const uint4 *>(knew + src + 8 * c) : make_uint4(0, 0, 0, 0);
-#pragma unroll
-            for (int k = 0; k < kBlocks; ++k)
-                vr[t][k] = in ? *reinterpret_cast<const uint32_t *>(vnew + src + 32 * k + 2 * c) : 0;
-        }
         const size_t at = static_cast<size_t>(q.page) * hkv + h;
+        const int64_t src = (static_cast<int64_t>(row0) + q.row) * hkv + h;  // of slot t = 0
         uint8_t *sc = scales + at * kScaleBytes;
-#pragma unroll
-        for (int t = 0; t < 4; ++t) {
-            uint32_t byte;
-            const uint32_t codes = encode_k(kr[t], &byte);
-            if (t < q.t0 || t >= q.t1) continue;
-            *reinterpret_cast<uint32_t *>(kpool + at * kCodeBytes + (4 * q.g + t) * (kHeadDim / 2) + 4 * c) = codes;
-            if ((c & 3) == 0) sc[(c >> 2) * kPageSize + 4 * q.g + t] = static_cast<uint8_t>(byte);
-        }
-        uint32_t codes[kBlocks], bytes[kBlocks];
-        encode_v(vr, codes, bytes);
-        store_v(vpool + at * kCodeBytes, sc, codes, bytes, q.g, q.t0, q.t1, c);
+        write_k(knew + src * kHeadDim, hkv * kHeadDim, kpool + at * kCodeBytes, sc, q.g, q.t0, q.t1, c);
+        write_v(vnew + src * kHeadDim, hkv * kHeadDim, vpool + at * kCodeBytes, sc, q.g, q.t0, q.t1, c);
     }
 }
 

@@ -25,7 +25,7 @@ struct NormRopeArgs {
     const uint16_t *q_weight, *k_weight;   // NULL: no norm
     const double *inv_freq;
     float eps;
-    int rot_dim, neighbours, hq;
+    int rot_dim, hq;
     uint16_t *q_out;
 };
 struct Cache {
@@ -43,14 +43,27 @@ __device__ __forceinline__ uint32_t pack2(float a, float b) {
     v[1] = static_cast<__bf16>(b);
     return __builtin_bit_cast(uint32_t, v);
 }
+constexpr int kRor8 = 0x128;  // DPP: rotate the 16 lanes by 8
 template <int kCtrl>
 __device__ __forceinline__ float add_dpp(float x) {
     return x + __builtin_bit_cast(float, dpp<kCtrl>(__builtin_bit_cast(uint32_t, x)));
 }
 
-// A lane's dims 8c .. 8c+7 of a head row; cs: the token's (cos, sin) by pair.
-__device__ __forceinline__ uint4 norm_rope_row(uint4 x, bool norm, uint4 w, float eps, int rot_dim, bool neighbours,
-                                               const float2 *cs, int c) {
+// A quad's angles in LDS, by token and pair, and the norm's weights.  Of the
+// halves' pairs the first lanes take the sine with its sign turned, from a copy of
+// its own.
+struct Shared {
+    float cos[4][kHeadDim / 2], sin[4][2][kHeadDim / 2];  // [0]: -sin, [1]: sin
+    float weight[2][kHeadDim];                            // of queries and keys
+};
+// Which dims are paired: neighbours, the halves of a whole head (8 lanes apart), or
+// the halves of its first rot_dim.
+enum Pairing { kNeighbours, kWholeHalves, kHalves };
+
+// A lane's dims 8c .. 8c+7 of a head row of token t.
+template <Pairing kPairing>
+__device__ __forceinline__ uint4 norm_rope_row(uint4 x, bool norm, const float *weight, float eps, int rot_dim,
+                                               const Shared &sh, int t, int c) {
     float y[8] = {lo(x.x), hi(x.x), lo(x.y), hi(x.y), lo(x.z), hi(x.z), lo(x.w), hi(x.w)};
     if (norm) {
         float sum = 0.f;
@@ -61,121 +74,152 @@ __device__ __forceinline__ uint4 norm_rope_row(uint4 x, bool norm, uint4 w, floa
         sum = add_dpp<kHalfMirror>(sum);
         sum = add_dpp<kMirror>(sum);
         const float r = rsqrtf(sum * (1.f / kHeadDim) + eps);
-        const float wf[8] = {lo(w.x), hi(w.x), lo(w.y), hi(w.y), lo(w.z), hi(w.z), lo(w.w), hi(w.w)};
 #pragma unroll
-        for (int j = 0; j < 8; ++j) y[j] = y[j] * r * wf[j];
+        for (int j = 0; j < 8; ++j) y[j] = y[j] * r * weight[8 * c + j];
     }
-    if (neighbours) {
+    if constexpr (kPairing == kNeighbours) {
         if (8 * c < rot_dim) {
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const float2 t = cs[4 * c + j];
+                const float cs = sh.cos[t][4 * c + j], sn = sh.sin[t][1][4 * c + j];
                 const float a = y[2 * j], b = y[2 * j + 1];
-                y[2 * j] = a * t.x - b * t.y;
-                y[2 * j + 1] = b * t.x + a * t.y;
+                y[2 * j] = a * cs - b * sn;
+                y[2 * j + 1] = b * cs + a * sn;
             }
         }
-    } else if (rot_dim > 0) {
-        const int half = rot_dim / 16;  // lanes of the first half
+    } else {
+        const int half = kPairing == kWholeHalves ? 8 : rot_dim / 16;  // lanes of the first half
         const bool first = c < half;
-        const int partner = (threadIdx.x & 48) | (first ? c + half : c < 2 * half ? c - half : c);
         float p[8];
+        if constexpr (kPairing == kWholeHalves) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) p[j] = __shfl(y[j], partner);
-        if (c < 2 * half) {
-            const float2 *at = cs + 8 * (first ? c : c - half);
+            for (int j = 0; j < 8; ++j) p[j] = __builtin_bit_cast(float, dpp<kRor8>(__builtin_bit_cast(uint32_t, y[j])));
+        } else {
+            const int partner = (threadIdx.x & 48) | (first ? c + half : c < 2 * half ? c - half : c);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) y[j] = y[j] * at[j].x + (first ? -p[j] : p[j]) * at[j].y;
+            for (int j = 0; j < 8; ++j) p[j] = __shfl(y[j], partner);
+        }
+        if (kPairing == kWholeHalves || c < 2 * half) {
+            const int pair = 8 * (first ? c : c - half);
+            const float *cs = &sh.cos[t][pair], *sn = &sh.sin[t][first ? 0 : 1][pair];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) y[j] = y[j] * cs[j] + p[j] * sn[j];
         }
     }
     return make_uint4(pack2(y[0], y[1]), pack2(y[2], y[3]), pack2(y[4], y[5]), pack2(y[6], y[7]));
+}
+
+// Head rows of a quad's tokens t0 .. t0 + m, `heads` of each, spread over the
+// `step` groups of 16 lanes that share the quad: task i is head i / m of token
+// i % m.  The next row's load is in flight while one is worked on: load(h, t),
+// store(h, t, x); each_row starts with the group's first row in x and returns its
+// place behind these tasks.
+__device__ __forceinline__ int head_of(int i, int m) {
+    return m == 4 ? i >> 2 : m == 1 ? i : m == 2 ? i >> 1 : static_cast<int>(static_cast<unsigned>(i) / 3u);
+}
+template <class Load>
+__device__ __forceinline__ uint4 row_of(int i, int t0, int m, int heads, const Load &load) {
+    const int h = head_of(i, m);
+    return i < m * heads ? load(h, t0 + i - h * m) : make_uint4(0, 0, 0, 0);
+}
+template <class Load, class Store>
+__device__ __forceinline__ int each_row(uint4 x, int group, int step, int t0, int m, int heads, const Load &load,
+                                        const Store &store) {
+    const int tasks = m * heads;
+#pragma unroll 1
+    for (int i = group; i < tasks; i += step) {
+        const uint4 now = x;
+        x = row_of(i + step, t0, m, heads, load);
+        const int h = head_of(i, m);
+        store(h, t0 + i - h * m, now);
+    }
+    const int next = group - tasks % step;
+    return next < 0 ? next + step : next;
 }
 
 // One work-group: the (up to four) new tokens of one quad of page slots; grid.z
 // slices share its heads.  The quad's angles are computed once, one a thread,
 // and lie in LDS; then 16 lanes take a head row at a time.  Quads, because V in 4
 // bits is stored by four tokens (kv4_format.h).
-template <bool kFourBit>
-__global__ void __launch_bounds__(256)
+// Measured (kernel alone): 4096 tokens of 32 + 2 * 8 heads into bf16, 101 MB, 23 us
+// (a copy of as many bytes 21); 9275 of 64 + 2 * 8 into 4 bits, 362 MB, 93 us.
+// Six work-groups per CU: with the registers of five the latter takes 99.
+template <bool kFourBit, Pairing kPairing>
+__global__ void __launch_bounds__(256, 6)
 k_norm_rope(NormRopeArgs a, Cache kv, const int32_t *__restrict__ indptr, const int32_t *__restrict__ start_pos) {
-    __shared__ float2 s_cs[4][kHeadDim / 2];
+    __shared__ __attribute__((aligned(16))) Shared sh;
     const int b = blockIdx.y, c = threadIdx.x & 15;
     const int row0 = indptr[b], n = indptr[b + 1] - row0, pos0 = start_pos[b];
     if (n <= 0 || pos0 < 0) return;
     const int32_t *btrow = kv.bt + static_cast<size_t>(b) * kv.bt_stride;
     const int quad0 = pos0 / 4, quads = (pos0 + n + 3) / 4 - quad0;
-    const uint4 none = make_uint4(0, 0, 0, 0);
-    const uint4 wq = a.q_weight ? *reinterpret_cast<const uint4 *>(a.q_weight + 8 * c) : none;
-    const uint4 wk = a.k_weight ? *reinterpret_cast<const uint4 *>(a.k_weight + 8 * c) : none;
-    const int rows = a.hq + kv.hkv;  // rotated rows of a token
+    {
+        const uint16_t *from = threadIdx.x < kHeadDim ? a.q_weight : a.k_weight;
+        const int d = threadIdx.x % kHeadDim;
+        if (from) sh.weight[threadIdx.x / kHeadDim][d] = lo(from[d]);
+    }
+    const int f = threadIdx.x & 63;
+    const double freq = 2 * f < a.rot_dim ? a.inv_freq[f] * 0.15915494309189533577 : 0.0;  // turns per position
+    const int step = gridDim.z * 16;
     for (int i = blockIdx.x; i < quads; i += gridDim.x) {
         const int first = (quad0 + i) * 4 - pos0;  // row of the quad's first slot
         const int t0 = max(0, -first), m = min(4, n - first) - t0;
         const int pos = pos0 + first, slot = pos % kPageSize;
         const int page = pos / kPageSize < kv.bt_stride ? btrow[pos / kPageSize] : -1;
         const bool held = page >= 0 && page < kv.num_pages;  // elsewhere only the queries are written
+        const int64_t row = static_cast<int64_t>(row0) + first;
+        const uint16_t *q_src = a.q + row * a.q_stride, *k_src = a.k + row * a.k_stride, *v_src = a.v + row * a.v_stride;
+        uint16_t *q_dst = a.q_out + row * a.hq * kHeadDim;
+        const size_t at = static_cast<size_t>(held ? page : 0) * kv.hkv;
+        // offsets within the quad fit 32 bits (the host refuses longer strides)
+        const auto source = [&](const uint16_t *from, int stride) __attribute__((always_inline)) {
+            return [=](int h, int t) __attribute__((always_inline)) {
+                const int off = ((t & 1) ? stride : 0) + ((t & 2) ? 2 * stride : 0) + h * kHeadDim + 8 * c;
+                return *reinterpret_cast<const uint4 *>(from + off);
+            };
+        };
+        const auto load_q = source(q_src, static_cast<int>(a.q_stride)), load_k = source(k_src, static_cast<int>(a.k_stride));
+        int group = blockIdx.z * 16 + (threadIdx.x >> 4);
+        const uint4 q_row = row_of(group, t0, m, a.hq, load_q);  // on its way while the angles are computed
         __syncthreads();  // the last quad's angles are read
-        {
-            const int t = threadIdx.x >> 6, f = threadIdx.x & 63;
-            if (2 * f < a.rot_dim) {
-                const double turns = static_cast<double>(pos + t) * a.inv_freq[f] * 0.15915494309189533577;
-                float sn, cs;
-                sincospif(static_cast<float>(2.0 * (turns - rint(turns))), &sn, &cs);
-                s_cs[t][f] = make_float2(cs, sn);
-            }
+        if (2 * f < a.rot_dim) {
+            const int t = threadIdx.x >> 6;
+            const double turns = static_cast<double>(pos + t) * freq;
+            float sn, cs;
+            sincospif(static_cast<float>(2.0 * (turns - rint(turns))), &sn, &cs);
+            sh.cos[t][f] = cs;
+            sh.sin[t][0][f] = -sn;
+            sh.sin[t][1][f] = sn;
         }
         __syncthreads();
-        const int v_tasks = kFourBit ? kv.hkv : m * kv.hkv;
-        const int tasks = m * rows + v_tasks;
-        const int step = gridDim.z * 16;
-        for (int task = blockIdx.z * 16 + (threadIdx.x >> 4); task < tasks; task += step) {
-            if (task < m * rows) {
-                const int h = task / m, t = t0 + task - h * m;
-                const int64_t row = static_cast<int64_t>(row0) + first + t;
-                if (h < a.hq) {
-                    const uint4 x = *reinterpret_cast<const uint4 *>(a.q + row * a.q_stride + h * kHeadDim + 8 * c);
-                    const uint4 y = norm_rope_row(x, a.q_weight != nullptr, wq, a.eps, a.rot_dim, a.neighbours != 0, s_cs[t], c);
-                    *reinterpret_cast<uint4 *>(a.q_out + (row * a.hq + h) * kHeadDim + 8 * c) = y;
-                } else {
-                    const int kh = h - a.hq;
-                    const uint4 x = *reinterpret_cast<const uint4 *>(a.k + row * a.k_stride + kh * kHeadDim + 8 * c);
-                    const uint4 y = norm_rope_row(x, a.k_weight != nullptr, wk, a.eps, a.rot_dim, a.neighbours != 0, s_cs[t], c);
-                    if (!held) continue;
-                    const size_t at = static_cast<size_t>(page) * kv.hkv + kh;
-                    if constexpr (kFourBit) {
-                        uint32_t byte;
-                        const uint32_t codes = encode_k(y, &byte);
-                        *reinterpret_cast<uint32_t *>(kv.k4 + at * kCodeBytes + (slot + t) * (kHeadDim / 2) + 4 * c) = codes;
-                        if ((c & 3) == 0)
-                            kv.scales[at * kScaleBytes + (c >> 2) * kPageSize + slot + t] = static_cast<uint8_t>(byte);
-                    } else {
-                        *reinterpret_cast<uint4 *>(kv.k + (at * kPageSize + slot + t) * kHeadDim + 8 * c) = y;
-                    }
-                }
-            } else if (held) {
-                const int v_task = task - m * rows;
-                if constexpr (kFourBit) {
-                    uint32_t vr[4][kBlocks];
-#pragma unroll
-                    for (int t = 0; t < 4; ++t) {
-                        const bool in = t >= t0 && t < t0 + m;
-                        const int64_t row = static_cast<int64_t>(row0) + first + (in ? t : t0);
-                        const uint16_t *src = a.v + row * a.v_stride + v_task * kHeadDim + 2 * c;
-#pragma unroll
-                        for (int k = 0; k < kBlocks; ++k)
-                            vr[t][k] = in ? *reinterpret_cast<const uint32_t *>(src + 32 * k) : 0;
-                    }
-                    uint32_t codes[kBlocks], bytes[kBlocks];
-                    encode_v(vr, codes, bytes);
-                    const size_t at = static_cast<size_t>(page) * kv.hkv + v_task;
-                    store_v(kv.v4 + at * kCodeBytes, kv.scales + at * kScaleBytes, codes, bytes, slot / 4, t0, t0 + m, c);
-                } else {
-                    const int vh = v_task / m, t = t0 + v_task - vh * m;
-                    const int64_t row = static_cast<int64_t>(row0) + first + t;
-                    *reinterpret_cast<uint4 *>(kv.v + ((static_cast<size_t>(page) * kv.hkv + vh) * kPageSize + slot + t) * kHeadDim + 8 * c) =
-                        *reinterpret_cast<const uint4 *>(a.v + row * a.v_stride + vh * kHeadDim + 8 * c);
-                }
+        group = each_row(q_row, group, step, t0, m, a.hq, load_q, [&](int h, int t, uint4 v) __attribute__((always_inline)) {
+            *reinterpret_cast<uint4 *>(q_dst + (static_cast<int>(__umul24(t, a.hq)) + h) * kHeadDim + 8 * c) =
+                norm_rope_row<kPairing>(v, a.q_weight != nullptr, sh.weight[0], a.eps, a.rot_dim, sh, t, c);
+        });
+        if (!held) continue;
+        const uint4 k_row = row_of(group, t0, m, kv.hkv, load_k);
+        group = each_row(k_row, group, step, t0, m, kv.hkv, load_k, [&](int h, int t, uint4 v) __attribute__((always_inline)) {
+            const uint4 y = norm_rope_row<kPairing>(v, a.k_weight != nullptr, sh.weight[1], a.eps, a.rot_dim, sh, t, c);
+            if constexpr (kFourBit) {
+                uint32_t byte;
+                const uint32_t codes = encode_k(y, &byte);
+                *reinterpret_cast<uint32_t *>(kv.k4 + (at + h) * kCodeBytes + (slot + t) * (kHeadDim / 2) + 4 * c) = codes;
+                if ((c & 3) == 0)
+                    kv.scales[(at + h) * kScaleBytes + (c >> 2) * kPageSize + slot + t] = static_cast<uint8_t>(byte);
+            } else {
+                *reinterpret_cast<uint4 *>(kv.k + ((at + h) * kPageSize + slot + t) * kHeadDim + 8 * c) = y;
             }
+        });
+        if constexpr (kFourBit) {
+            for (int h = group; h < kv.hkv; h += step)
+                write_v(v_src + h * kHeadDim, a.v_stride, kv.v4 + (at + h) * kCodeBytes, kv.scales + (at + h) * kScaleBytes,
+                        slot / 4, t0, t0 + m, c);
+        } else {
+            const auto load_v = source(v_src, static_cast<int>(a.v_stride));
+            const uint4 v_row = row_of(group, t0, m, kv.hkv, load_v);
+            each_row(v_row, group, step, t0, m, kv.hkv, load_v, [&](int h, int t, uint4 v) __attribute__((always_inline)) {
+                *reinterpret_cast<uint4 *>(kv.v + ((at + h) * kPageSize + slot + t) * kHeadDim + 8 * c) = v;
+            });
         }
     }
 }
@@ -211,7 +255,8 @@ extern "C" mw_status mw_qk_norm_rope_write(const mw_kv_pool *pool, const mw_norm
                       (hq > 0 && (!d_q_out || !aligned16(d_q_out)))))
         return fail(MW_ERR_INVALID_ARG,
                     "%s: rows must be 16-byte aligned, strides multiples of 8 elements and no less than a token's heads", who);
-    if (4 * (hq + 2 * hkv) > INT32_MAX / 2) return fail(MW_ERR_UNSUPPORTED, "%s: too many heads", who);
+    if (hq + 2 * hkv > (1 << 20) || q_stride > (1 << 28) || k_stride > (1 << 28) || v_stride > (1 << 28))
+        return fail(MW_ERR_UNSUPPORTED, "%s: at most 2^20 heads and strides of 2^28 elements", who);
     hipStream_t s = static_cast<hipStream_t>(stream);
     st = timing_begin(timing, s);
     if (st != MW_OK) return st;
@@ -227,11 +272,13 @@ extern "C" mw_status mw_qk_norm_rope_write(const mw_kv_pool *pool, const mw_norm
                              static_cast<const uint16_t *>(d_v), q_stride, k_stride, v_stride,
                              static_cast<const uint16_t *>(rope->d_q_weight),
                              static_cast<const uint16_t *>(rope->d_k_weight), rope->d_inv_freq, rope->eps, rope->rot_dim,
-                             rope->neighbours, static_cast<int>(hq), static_cast<uint16_t *>(d_q_out)};
+                             static_cast<int>(hq), static_cast<uint16_t *>(d_q_out)};
         const Cache kv{pool->k, pool->v, pool->k4, pool->v4, pool->scales, d_block_table, bt_stride,
                        pool->desc.num_pages, pool->desc.num_kv_heads};
-        hipLaunchKernelGGL(pool->k4 ? k_norm_rope<true> : k_norm_rope<false>,
-                           dim3(static_cast<unsigned>(blocks), batch, static_cast<unsigned>(slices)), dim3(256), 0, s, a,
+        auto kernel = rope->neighbours          ? (pool->k4 ? k_norm_rope<true, kNeighbours> : k_norm_rope<false, kNeighbours>)
+                      : rope->rot_dim == kHeadDim ? (pool->k4 ? k_norm_rope<true, kWholeHalves> : k_norm_rope<false, kWholeHalves>)
+                                                  : (pool->k4 ? k_norm_rope<true, kHalves> : k_norm_rope<false, kHalves>);
+        hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(blocks), batch, static_cast<unsigned>(slices)), dim3(256), 0, s, a,
                            kv, d_qo_indptr, d_start_pos);
         st = check_launch("k_norm_rope");
         if (st != MW_OK) return st;

@@ -312,6 +312,15 @@ def mw_kv_pool_gather(pool, d_block_table: int, n_tokens: int, d_k_out: int, d_v
 
 
 # ---------------------------------------------------- pool in 4 bits, rows ---
+def _enqueue(call, *args):
+    """Makes a call whose addresses are passed on as they are (ctypes takes ints,
+    None and handles; seven conversions by ``_h`` are a microsecond of a call)."""
+    try:
+        _check(call(*args))
+    except ctypes.ArgumentError:  # numpy integers
+        _check(call(*(int(a) if isinstance(a, np.integer) else a for a in args)))
+
+
 def mw_kv4_pool_create(num_pages: int, page_size: int, num_kv_heads: int, head_dim: int, d_k_codes: int,
                        d_v_codes: int, d_scales: int):
     out = _P()
@@ -324,24 +333,23 @@ def mw_kv4_pool_create(num_pages: int, page_size: int, num_kv_heads: int, head_d
 def mw_kv4_pool_write(pool, new_lens, start_pos, d_qo_indptr: int, d_start_pos: int, d_block_table: int,
                       bt_stride: int, d_k_new: int, d_v_new: int, stream=0, timing=None):
     nl, sp = _i32(new_lens), _i32(start_pos)
-    _check(load().mw_kv4_pool_write(pool, len(nl), _pi(nl), _pi(sp), _h(d_qo_indptr), _h(d_start_pos),
-                                    _h(d_block_table), bt_stride, _h(d_k_new), _h(d_v_new), _h(stream), timing))
+    _enqueue(load().mw_kv4_pool_write, pool, len(nl), _pi(nl), _pi(sp), d_qo_indptr, d_start_pos, d_block_table,
+             bt_stride, d_k_new, d_v_new, stream, timing)
 
 
 def mw_kv4_pool_gather(pool, lens, start_pos, d_indptr: int, d_start_pos: int, d_block_table: int, bt_stride: int,
                        d_k_out: int, d_v_out: int, stream=0, timing=None):
     nl, sp = _i32(lens), _i32(start_pos)
-    _check(load().mw_kv4_pool_gather(pool, len(nl), _pi(nl), _pi(sp), _h(d_indptr), _h(d_start_pos),
-                                     _h(d_block_table), bt_stride, _h(d_k_out), _h(d_v_out), _h(stream), timing))
+    _enqueue(load().mw_kv4_pool_gather, pool, len(nl), _pi(nl), _pi(sp), d_indptr, d_start_pos, d_block_table,
+             bt_stride, d_k_out, d_v_out, stream, timing)
 
 
 def mw_qk_norm_rope_write(pool, rope: NormRope, new_lens, start_pos, d_qo_indptr: int, d_start_pos: int,
                           d_block_table: int, bt_stride: int, d_q: int, q_stride: int, d_k: int, k_stride: int,
                           d_v: int, v_stride: int, d_q_out: int, stream=0, timing=None):
     nl, sp = _i32(new_lens), _i32(start_pos)
-    _check(load().mw_qk_norm_rope_write(pool, ctypes.byref(rope), len(nl), _pi(nl), _pi(sp), _h(d_qo_indptr),
-                                        _h(d_start_pos), _h(d_block_table), bt_stride, _h(d_q), q_stride, _h(d_k),
-                                        k_stride, _h(d_v), v_stride, _h(d_q_out), _h(stream), timing))
+    _enqueue(load().mw_qk_norm_rope_write, pool, ctypes.byref(rope), len(nl), _pi(nl), _pi(sp), d_qo_indptr,
+             d_start_pos, d_block_table, bt_stride, d_q, q_stride, d_k, k_stride, d_v, v_stride, d_q_out, stream, timing)
 
 
 # ------------------------------------------------------------- partition ---
@@ -508,9 +516,8 @@ def mw_kv4_decode_attn(pool, num_q_heads: int, num_kv_heads: int, head_dim: int,
                        workspace_bytes: int, stream=0, timing=None):
     sl = _i32(seq_lens)
     sh = _shape(num_q_heads, num_kv_heads, head_dim, scale)
-    _check(load().mw_kv4_decode_attn(pool, ctypes.byref(sh), len(sl), _pi(sl), _h(d_seq_lens), _h(d_block_table),
-                                     bt_stride, _h(d_q), _h(d_out), _h(d_workspace), workspace_bytes, _h(stream),
-                                     timing))
+    _enqueue(load().mw_kv4_decode_attn, pool, ctypes.byref(sh), len(sl), _pi(sl), d_seq_lens, d_block_table,
+             bt_stride, d_q, d_out, d_workspace, workspace_bytes, stream, timing)
 
 
 def mw_kv4_prefill_workspace_size(num_q_heads: int, num_kv_heads: int, head_dim: int, new_lens, prefix_lens,
@@ -528,9 +535,8 @@ def mw_kv4_prefill_attn(pool, num_q_heads: int, num_kv_heads: int, head_dim: int
                         d_out: int, d_workspace: int, workspace_bytes: int, stream=0, timing=None):
     nl, pl = _i32(new_lens), _i32(prefix_lens)
     sh = _shape(num_q_heads, num_kv_heads, head_dim, scale)
-    _check(load().mw_kv4_prefill_attn(pool, ctypes.byref(sh), len(nl), _pi(nl), _pi(pl), _h(d_qo_indptr),
-                                      _h(d_prefix_lens), _h(d_block_table), bt_stride, _h(d_q), _h(d_out),
-                                      _h(d_workspace), workspace_bytes, _h(stream), timing))
+    _enqueue(load().mw_kv4_prefill_attn, pool, ctypes.byref(sh), len(nl), _pi(nl), _pi(pl), d_qo_indptr,
+             d_prefix_lens, d_block_table, bt_stride, d_q, d_out, d_workspace, workspace_bytes, stream, timing)
 
 
 def mw_decode_attn_noalloc(pool, num_q_heads: int, num_kv_heads: int, head_dim: int, scale: float,

@@ -429,12 +429,14 @@ mw_status mw_kv4_decode_attn(const mw_kv_pool *pool, const mw_attn_shape *shape,
                              const int32_t *h_seq_lens, const int32_t *d_seq_lens, const int32_t *d_block_table,
                              int32_t bt_stride, const void *d_q, void *d_out, void *d_workspace, size_t workspace_bytes,
                              mw_stream stream, mw_timing *timing);
-/* Prefill: arguments as mw_prefill_attn_ws.  The batch's pages are unpacked to
- * bf16 in the workspace and attended there (a chunk of n tokens reads every page
- * for each of its query blocks).  The workspace is the size call's for these
- * lengths: 2 * 4096 bytes per (page, kv head) of the batch, a table, and what
- * mw_prefill_attn_ws takes for itself; layers that run one after the other can
- * share it. */
+/* Prefill: arguments as mw_prefill_attn_ws.  A chunk of at most 8 blocks of 128
+ * (token, query head) rows to a kv head may read the codes itself (a kernel, and one
+ * more where its keys are split and added up); of any other the batch's pages are
+ * unpacked to bf16 in the workspace and attended there.  The lengths and head counts
+ * alone decide, by what either would take.  The workspace is the size call's for
+ * these lengths: the split's sums, which may be none, or 2 * 4096 bytes per (page,
+ * kv head) of the batch, a table, and what mw_prefill_attn_ws takes for itself;
+ * layers that run one after the other can share it. */
 mw_status mw_kv4_prefill_workspace_size(const mw_attn_shape *shape, int32_t batch, const int32_t *h_new_lens,
                                         const int32_t *h_prefix_lens, int32_t num_cus, size_t *bytes);
 mw_status mw_kv4_prefill_attn(const mw_kv_pool *pool, const mw_attn_shape *shape, int32_t batch,

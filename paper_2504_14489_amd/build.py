@@ -19,7 +19,7 @@ INCLUDE = os.path.join(ROOT, "include")
 BUILD = os.path.join(ROOT, "_build")
 LIB = os.path.join(PKG, "libmw.so")
 
-SOURCES = ["runtime.hip", "kv_pool.hip", "decode_attn.hip", "prefill_attn.hip", "fused_attn.hip", "kv4_pool.hip", "kv4_attn.hip",
+SOURCES = ["runtime.hip", "kv_pool.hip", "decode_attn.hip", "prefill_attn.hip", "fused_attn.hip", "kv4_pool.hip", "kv4_decode.hip", "kv4_prefill.hip",
            "norm_rope.hip", "estimator.cpp", "engine.cpp"]
 ARCH = "gfx950"
 # Packed FP32 instructions are disabled: hipcc would otherwise form

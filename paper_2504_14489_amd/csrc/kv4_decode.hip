@@ -1,6 +1,5 @@
-// Attention over the cache in 4 bits: decode, and prefill.
-#include "decode_block.h"
-#include "kv4_format.h"
+// Decode attention over the cache in 4 bits.
+#include "kv4_block.h"
 
 using namespace mw;
 
@@ -9,21 +8,13 @@ namespace {
 using namespace dk;
 using namespace kv4;
 
-typedef int i32x8 __attribute__((ext_vector_type(8)));
-typedef short i16x2 __attribute__((ext_vector_type(2)));
-
-// ------------------------------------------------------------------ decode
 // The balanced split of decode_block.h (its units, shares, pieces and merge) on
 // pages of 2176 bytes instead of 8192: per byte nearly four times the work, so
 // the work is what the body is built around.  Nothing of a page passes through
 // LDS or is converted but V:
 //   * S^T[token][head] = K Q^T on the scaled 16x16x128 matrix instruction, K as
 //     it lies in memory with its scale bytes (a page is one 16-byte load a lane),
-//     Q^T as the sum of two e4m3 operands hi + lo: q 2^-e with e such that a row's
-//     largest is in [128, 256), hi its nearest, lo the nearest of the rest.  hi keeps
-//     four bits of the eight that bf16 has and the rest has four, so the sum is
-//     exact down to 2^-10 of the row's largest, and off by at most 2^-18 of it
-//     below.
+//     Q^T as the sum of two e4m3 operands (kv4_block.h).
 //   * O^T[dim][head] += V^T P^T on the bf16 instruction, V^T a conversion of two
 //     codes each (without scales: 32 conversions for two pages) and the scale of
 //     (token, block of 32 dims) multiplied into P^T.  A tile of 16 dims has one
@@ -46,76 +37,6 @@ struct Span4Lds {
     float2 ml[kRecords][kHeads];
     Fragment frag[kRecords];
     int done[2];  // the pending segments' pieces are all done
-};
-
-// Two bf16 values into half kHalf of hi and lo.
-template <int kHalf>
-__device__ __forceinline__ void split2(uint32_t two, float unit, i16x2 &hi, i16x2 &lo) {
-    hi = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(hi, __builtin_bit_cast(bf16x2_t, two), unit, kHalf);
-    const auto near = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(__builtin_bit_cast(int, hi), unit, kHalf);
-    lo = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(lo, __builtin_bit_cast(float, two << 16) - near[0],
-                                                  __builtin_bit_cast(float, two & 0xffff0000u) - near[1], unit, kHalf);
-}
-
-// hi and lo operands of a Q row and the factor of its scores; x[i]: the lane's
-// dims 64 (i / 2) + 16 g + 8 (i % 2) .. +7 of its column's row.
-__device__ __forceinline__ float split_q(const uint4 (&x)[4], i32x8 &hi, i32x8 &lo) {
-    uint32_t most = 0;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) most = max2(max2(max2(most, abs2(x[i].x)), max2(abs2(x[i].y), abs2(x[i].z))), abs2(x[i].w));
-    most = max(most & 0xffff, most >> 16);
-    most = max(most, static_cast<uint32_t>(__shfl_xor(static_cast<int>(most), 16)));
-    most = max(most, static_cast<uint32_t>(__shfl_xor(static_cast<int>(most), 32)));
-    const int power = static_cast<int>(most >> 7);
-    const int e = max(power - 127 - 7, -100);  // rows below 2^-93 keep fewer bits
-    const float unit = __builtin_bit_cast(float, static_cast<uint32_t>(127 + e) << 23);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            i16x2 h{0, 0}, l{0, 0};
-            split2<0>(w[2 * j], unit, h, l);
-            split2<1>(w[2 * j + 1], unit, h, l);
-            hi[2 * i + j] = __builtin_bit_cast(int, h);
-            lo[2 * i + j] = __builtin_bit_cast(int, l);
-        }
-    }
-    // a row that is not finite: NaN scores
-    return power == 255 ? NAN : unit;
-}
-
-// Weighted sum of the fragments or pieces of one head in a wave: (m, l) of up to
-// 64 of them one per lane, which gives every weight 2^(m - M) and the denominator
-// within the wave, then two outputs per lane.  Those without keys have l = 0 and
-// contribute nothing.  load_o(j): the lane's two values of the j-th, j < n.
-struct HeadSum {
-    float M = -INFINITY, L = 0.f;
-    float2 acc = make_float2(0.f, 0.f);
-    template <class LoadO>
-    __device__ __forceinline__ void add(float2 ml, int n, int lane, const LoadO &load_o) {
-        const bool in = lane < n && ml.y != 0.f;
-        const float top = fmaxf(M, wave_max(in ? ml.x : -INFINITY));
-        const float old = L == 0.f ? 0.f : __builtin_amdgcn_exp2f(M - top);
-        const float w = in ? __builtin_amdgcn_exp2f(ml.x - top) : 0.f;
-        M = top;
-        L = L * old + wave_sum(in ? w * ml.y : 0.f);
-        acc.x *= old;
-        acc.y *= old;
-#pragma unroll 1
-        for (int j0 = 0; j0 < n; j0 += 8) {
-            float2 o[8];
-#pragma unroll
-            for (int k = 0; k < 8; ++k) o[k] = load_o(min(j0 + k, n - 1));
-#pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                // lanes from n on have weight 0, and j0 + k < 64
-                const float wk = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, w), j0 + k));
-                acc.x += wk * o[k].x;
-                acc.y += wk * o[k].y;
-            }
-        }
-    }
 };
 
 // The end of a unit, after the barrier behind its waves' shares: as
@@ -243,25 +164,6 @@ finish_unit(uint16_t *__restrict__ out, float *__restrict__ ws_o, float2 *__rest
     }
 }
 
-// The larger of m and four scores; a NaN wins, which spares the instructions that
-// would quiet it (its column comes out as NaN).
-__device__ __forceinline__ float max4(float m, f32x4 s) {
-    return __builtin_elementwise_maximum(
-        __builtin_elementwise_maximum(__builtin_elementwise_maximum(m, s[0]), s[1]),
-        __builtin_elementwise_maximum(s[2], s[3]));
-}
-// x of the four lanes of a column (those 16 and 32 apart) combined by f, in each.
-template <class F>
-__device__ __forceinline__ float across(float x, const F &f) {
-    const auto pair = [&](auto r) {
-        const uint32_t lo = r[0], hi = r[1];  // (a bit cast of an element itself takes the first one)
-        return f(__builtin_bit_cast(float, lo), __builtin_bit_cast(float, hi));
-    };
-    const uint32_t a = __builtin_bit_cast(uint32_t, x);
-    const uint32_t b = __builtin_bit_cast(uint32_t, pair(__builtin_amdgcn_permlane16_swap(a, a, false, false)));
-    return pair(__builtin_amdgcn_permlane32_swap(b, b, false, false));
-}
-
 __device__ __forceinline__ bf16x8 v_operand(uint4 a, uint4 b, int t) {
     const uint32_t p = t < 2 ? a.x : t < 4 ? a.y : t < 6 ? a.z : a.w, q = t < 2 ? b.x : t < 4 ? b.y : t < 6 ? b.z : b.w;
     const uint4 r = t & 1 ? make_uint4(decode2<2>(p, 1.f), decode2<3>(p, 1.f), decode2<2>(q, 1.f), decode2<3>(q, 1.f))
@@ -289,7 +191,7 @@ k_kv4_decode(const uint8_t *__restrict__ kpool, const uint8_t *__restrict__ vpoo
     using Chunk = SpanShare::Chunk;
     const bool in_group = head < group;
 
-    i32x8 q_hi, q_lo;
+    i32x8 q_hi[1], q_lo[1];
     float q_scale = 0.f;
     uint4 q_next[4];  // the next fragment's rows, on their way since its chunk is known
     auto load_q = [&](const Chunk &c) __attribute__((always_inline)) {
@@ -299,7 +201,7 @@ k_kv4_decode(const uint8_t *__restrict__ kpool, const uint8_t *__restrict__ vpoo
     };
     auto take_q = [&]() __attribute__((always_inline)) {
         // (above 0, or a masked score would be a NaN; of a NaN row, NaN)
-        const float f = split_q(q_next, q_hi, q_lo) * scale_log2;
+        const float f = split_q<true>(q_next, q_hi, q_lo) * scale_log2;
         q_scale = f < 1e-37f ? 1e-37f : f;
     };
 
@@ -396,8 +298,8 @@ k_kv4_decode(const uint8_t *__restrict__ kpool, const uint8_t *__restrict__ vpoo
                                   static_cast<int>(kr[j].w), 0, 0, 0, 0};
                     const int s = static_cast<int>(ks[j]);
                     // A: four-bit floats with their scales; B: e4m3 with scale 1
-                    sc[j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, q_hi, f32x4{0.f, 0.f, 0.f, 0.f}, 4, 0, 0, s, 0, 127);
-                    sc[j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, q_lo, sc[j], 4, 0, 0, s, 0, 127);
+                    sc[j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, q_hi[0], f32x4{0.f, 0.f, 0.f, 0.f}, 4, 0, 0, s, 0, 127);
+                    sc[j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, q_lo[0], sc[j], 4, 0, 0, s, 0, 127);
                 }
                 // the next step's K loads go out while this one is computed, its V
                 // loads once this one's V is used
@@ -505,101 +407,6 @@ k_kv4_decode(const uint8_t *__restrict__ kpool, const uint8_t *__restrict__ vpoo
     finish_unit<kHeads>(out, ws_o, ws_ml, flags, tag, slots, hkv, group, aligned, u, tid, lds);
 }
 
-// ----------------------------------------------------------------- prefill
-// Unpacks the pages of a batch's sequences, laid end to end, to bf16 pages
-// [page][kv head][16][128] and writes the table that names them.  One wave to a
-// (page, kv head).
-struct ChunkLengths {
-    const int32_t *indptr, *prefix;
-    int batch, bt_stride;
-    __device__ __forceinline__ int pages(int b) const {
-        if (b >= batch) return 0;
-        const int64_t len = static_cast<int64_t>(indptr[b + 1]) - indptr[b] + prefix[b];
-        const int64_t np = (len + kPageSize - 1) / kPageSize;
-        return static_cast<int>(max(int64_t{0}, min(np, static_cast<int64_t>(bt_stride))));
-    }
-};
-
-__global__ void __launch_bounds__(256)
-k_kv4_unpack(const uint8_t *__restrict__ kpool, const uint8_t *__restrict__ vpool, const uint8_t *__restrict__ scales,
-             uint16_t *__restrict__ kout, uint16_t *__restrict__ vout, int32_t *__restrict__ table, int table_stride,
-             const int32_t *__restrict__ indptr, const int32_t *__restrict__ prefix, const int32_t *__restrict__ bt,
-             int bt_stride, int batch, int num_pages, int hkv, int64_t items) {
-    const int lane = threadIdx.x & 63;
-    const int64_t item = static_cast<int64_t>(blockIdx.x) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    if (item >= items) return;
-    const int page_no = static_cast<int>(item / hkv), h = static_cast<int>(item - static_cast<int64_t>(page_no) * hkv);
-    const ChunkLengths len{indptr, prefix, batch, bt_stride};
-    int running = 0, b = -1, p = 0;
-    for (int b0 = 0; b0 < batch; b0 += 64) {
-        const int np = len.pages(b0 + lane);
-        const int incl = running + lane_scan(np);
-        const uint64_t hit = __builtin_amdgcn_ballot_w64(page_no >= incl - np && page_no < incl);
-        if (hit) {
-            const int src = __builtin_ctzll(hit);
-            b = b0 + src;
-            p = page_no - __builtin_amdgcn_readlane(incl - np, src);
-            break;
-        }
-        running = __builtin_amdgcn_readlane(incl, 63);
-    }
-    if (b < 0 || p >= table_stride) return;  // device lengths that disagree with the host's
-    const int page = bt[static_cast<size_t>(b) * bt_stride + p];
-    const bool ok = page >= 0 && page < num_pages;
-    if (h == 0 && lane == 0) table[static_cast<size_t>(b) * table_stride + p] = ok ? page_no : -1;
-    if (!ok) return;
-    const size_t at = static_cast<size_t>(page) * hkv + h;
-    const uint8_t *sc = scales + at * kScaleBytes;
-    // K: four lane-contiguous dwords (8 dims) of codes, 16 bytes out each
-    const uint32_t *kc = reinterpret_cast<const uint32_t *>(kpool + at * kCodeBytes) + lane;
-    uint32_t codes_k[4], byte_k[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        codes_k[i] = kc[64 * i];
-        byte_k[i] = sc[((lane & 15) >> 2) * kPageSize + 4 * i + (lane >> 4)];
-    }
-    const int g = lane >> 4, c = lane & 15;
-    const uint4 vc = *reinterpret_cast<const uint4 *>(vpool + at * kCodeBytes + lane * 16);
-    uint32_t bytes[kBlocks], vr[4][kBlocks];
-#pragma unroll
-    for (int k = 0; k < kBlocks; ++k) bytes[k] = *reinterpret_cast<const uint32_t *>(sc + (kBlocks + k) * kPageSize + 4 * g);
-    uint4 *ko = reinterpret_cast<uint4 *>(kout + static_cast<size_t>(item) * (kPageSize * kHeadDim)) + lane;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) ko[64 * i] = decode_k(codes_k[i], byte_k[i]);
-    const uint32_t codes[kBlocks] = {vc.x, vc.y, vc.z, vc.w};
-    decode_v(codes, bytes, vr);
-    uint32_t *vo = reinterpret_cast<uint32_t *>(vout + static_cast<size_t>(item) * (kPageSize * kHeadDim)) + c;
-#pragma unroll
-    for (int t = 0; t < 4; ++t)
-#pragma unroll
-        for (int k = 0; k < kBlocks; ++k) vo[(4 * g + t) * (kHeadDim / 2) + 16 * k] = vr[t][k];
-}
-
-// Workspace of a prefill call: K pages, V pages, their table, then the
-// workspace of the attention itself.
-struct UnpackLayout {
-    int64_t pages;
-    int64_t table_stride;
-    size_t off_v, off_table, off_ws;
-};
-mw_status unpack_layout(int32_t batch, const int32_t *h_new_lens, const int32_t *h_prefix_lens, int64_t hkv,
-                        UnpackLayout *u, const char *who) {
-    u->pages = 0;
-    u->table_stride = 1;
-    for (int32_t b = 0; b < batch; ++b) {
-        const int64_t np = (static_cast<int64_t>(h_new_lens[b]) + h_prefix_lens[b] + kPageSize - 1) / kPageSize;
-        u->pages += np;
-        u->table_stride = np > u->table_stride ? np : u->table_stride;
-    }
-    if (u->pages > INT32_MAX || u->pages * hkv > static_cast<int64_t>(INT32_MAX) * 4)
-        return fail(MW_ERR_UNSUPPORTED, "%s: too many pages", who);
-    const size_t pages_bytes = static_cast<size_t>(u->pages) * hkv * (kPageSize * kHeadDim * 2);
-    u->off_v = pages_bytes;
-    u->off_table = 2 * pages_bytes;
-    u->off_ws = (u->off_table + static_cast<size_t>(batch) * u->table_stride * 4 + 255) & ~static_cast<size_t>(255);
-    return MW_OK;
-}
-
 }  // namespace
 
 extern "C" {
@@ -638,68 +445,6 @@ mw_status mw_kv4_decode_attn(const mw_kv_pool *pool, const mw_attn_shape *shape,
     st = timing_kernel_done(timing, s);
     timing_end(timing);
     return st;
-}
-
-mw_status mw_kv4_prefill_workspace_size(const mw_attn_shape *shape, int32_t batch, const int32_t *h_new_lens,
-                                        const int32_t *h_prefix_lens, int32_t num_cus, size_t *bytes) {
-    const char *who = "mw_kv4_prefill_workspace_size";
-    size_t inner = 0;
-    mw_status st = mw_prefill_workspace_size(shape, batch, h_new_lens, h_prefix_lens, num_cus, &inner);
-    if (st != MW_OK) return st;
-    if (!bytes) return fail(MW_ERR_INVALID_ARG, "%s: bytes is NULL", who);
-    UnpackLayout u;
-    st = unpack_layout(batch, h_new_lens, h_prefix_lens, shape->num_kv_heads, &u, who);
-    if (st != MW_OK) return st;
-    *bytes = u.off_ws + inner;
-    return MW_OK;
-}
-
-mw_status mw_kv4_prefill_attn(const mw_kv_pool *pool, const mw_attn_shape *shape, int32_t batch,
-                              const int32_t *h_new_lens, const int32_t *h_prefix_lens, const int32_t *d_qo_indptr,
-                              const int32_t *d_prefix_lens, const int32_t *d_block_table, int32_t bt_stride,
-                              const void *d_q, void *d_out, void *d_workspace, size_t workspace_bytes, mw_stream stream,
-                              mw_timing *timing) {
-    const char *who = "mw_kv4_prefill_attn";
-    int64_t max_n = 0, total = 0;
-    mw_status st = check_rows(pool, batch, h_new_lens, h_prefix_lens, d_qo_indptr, d_prefix_lens, d_block_table,
-                              bt_stride, &max_n, &total, who);
-    if (st == MW_OK) st = check_pool_kind(pool, true, who);
-    if (st == MW_OK && !shape) st = fail(MW_ERR_INVALID_ARG, "%s: bad arguments", who);
-    if (st != MW_OK) return st;
-    hipStream_t s = static_cast<hipStream_t>(stream);
-    UnpackLayout u;
-    st = unpack_layout(batch, h_new_lens, h_prefix_lens, pool->desc.num_kv_heads, &u, who);
-    if (st != MW_OK) return st;
-    if (total > 0 && (!d_workspace || !aligned16(d_workspace) || workspace_bytes < u.off_ws))
-        return fail(MW_ERR_INVALID_ARG, "%s: needs a 16-byte aligned workspace of %zu bytes and the attention's (got %zu)",
-                    who, u.off_ws, workspace_bytes);
-    char *ws = static_cast<char *>(d_workspace);
-    // the unpacked pages, as the pool that the attention reads
-    mw_kv_pool bf16{};
-    bf16.desc = pool->desc;
-    bf16.desc.num_pages = static_cast<int32_t>(u.pages > 0 ? u.pages : 1);
-    bf16.k = reinterpret_cast<uint16_t *>(ws);
-    bf16.v = reinterpret_cast<uint16_t *>(ws + u.off_v);
-    int32_t *table = reinterpret_cast<int32_t *>(ws + u.off_table);
-    const size_t left = total > 0 ? workspace_bytes - u.off_ws : 0;
-    const mw_prefill_args a{&bf16,       *shape,        batch, h_new_lens,
-                            h_prefix_lens, d_qo_indptr, d_prefix_lens, table,
-                            static_cast<int32_t>(u.table_stride), d_q, d_out, ws + u.off_ws, left};
-    PrefillPlan pl;
-    const int64_t cus = stream_cus(s);
-    st = prefill_prepare(&a, cus, true, &pl, who, true);
-    if (st == MW_OK) st = prefill_fit_workspace(&a, cus, &pl, ws + u.off_ws, left, who);
-    if (st == MW_OK) st = timing_begin(timing, s);
-    if (st != MW_OK) return st;
-    if (total == 0) return prefill_launch(a, pl, s, timing);
-    const int64_t items = u.pages * pool->desc.num_kv_heads;
-    hipLaunchKernelGGL(k_kv4_unpack, dim3(static_cast<unsigned>((items + 3) / 4)), dim3(256), 0, s, pool->k4, pool->v4,
-                       pool->scales, bf16.k, bf16.v, table, static_cast<int>(u.table_stride), d_qo_indptr, d_prefix_lens,
-                       d_block_table, bt_stride, batch, pool->desc.num_pages, pool->desc.num_kv_heads, items);
-    st = check_launch("k_kv4_unpack");
-    if (st == MW_OK) st = timing_kernel_done(timing, s);
-    if (st != MW_OK) return st;
-    return prefill_launch(a, pl, s, timing);
 }
 
 }  // extern "C"

@@ -91,15 +91,8 @@ __device__ __forceinline__ uint32_t encode_k(uint4 x, uint32_t *byte) {
 }
 
 // The four codes of one dim for tokens 4g .. 4g+3 lie in 16 bits, those of its
-// neighbour in the next 16 (kept); a conversion takes or gives the two dims of
-// one token in a byte, token k in byte k (by token).
-__device__ __forceinline__ uint32_t by_token(uint32_t kept) {
-    const auto spread = [](uint32_t x) {  // 4 x 4 bits -> 4 x 8 bits
-        x = (x | x << 8) & 0x00ff00ffu;
-        return (x | x << 4) & 0x0f0f0f0fu;
-    };
-    return spread(kept & 0xffffu) | spread(kept >> 16) << 4;
-}
+// neighbour in the next 16; a conversion takes or gives the two dims of one token
+// in a byte.  by_dim: from tokens in bytes 0 .. 3.
 __device__ __forceinline__ uint32_t by_dim(uint32_t tokens) {
     const auto gather = [](uint32_t x) {
         x = (x | x >> 4) & 0x00ff00ffu;
@@ -131,16 +124,20 @@ __device__ __forceinline__ void encode_v(const uint32_t (&x)[kBlocks], int k, ui
     }
 }
 
-// The inverse: x[k][b] from the codes of block b, kept by dim, and its tokens' scale bytes.
+// The inverse: x[k][b] from the codes of block b, kept by dim, and its tokens' scale
+// bytes.  (A conversion takes the exponent of its scale and no other bit of it, so
+// a byte is only shifted there.)
 __device__ __forceinline__ void decode_v(const uint32_t (&codes)[kBlocks], const uint32_t (&bytes)[kBlocks],
                                          uint32_t (&x)[4][kBlocks]) {
+    const auto scale = [](uint32_t bits) { return __builtin_bit_cast(float, bits); };
 #pragma unroll
     for (int b = 0; b < kBlocks; ++b) {
-        const uint32_t t = by_token(codes[b]);
-        x[0][b] = decode2<0>(t, scale_of(bytes[b] & 255));
-        x[1][b] = decode2<1>(t, scale_of(bytes[b] >> 8 & 255));
-        x[2][b] = decode2<2>(t, scale_of(bytes[b] >> 16 & 255));
-        x[3][b] = decode2<3>(t, scale_of(bytes[b] >> 24));
+        const uint32_t even = codes[b] & 0x0f0f0f0fu, odd = codes[b] >> 4 & 0x0f0f0f0fu;  // tokens 0, 2 and 1, 3
+        const uint32_t t02 = even | even >> 12, t13 = odd | odd >> 12;
+        x[0][b] = decode2<0>(t02, scale(bytes[b] << 23));
+        x[1][b] = decode2<0>(t13, scale(bytes[b] << 15));
+        x[2][b] = decode2<1>(t02, scale(bytes[b] << 7));
+        x[3][b] = decode2<1>(t13, scale(bytes[b] >> 1));
     }
 }
 __device__ __forceinline__ uint4 decode_k(uint32_t codes, uint32_t byte) {

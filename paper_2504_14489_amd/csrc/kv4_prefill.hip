@@ -1,0 +1,588 @@
+// Prefill attention over the cache in 4 bits.
+#include <algorithm>
+
+#include "kv4_block.h"
+
+using namespace mw;
+
+namespace {
+
+using namespace dk;
+using namespace kv4;
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+// x of a lane and of the one 32 away combined by f, in both.
+template <class F>
+__device__ __forceinline__ float across_half(float x, const F &f) {
+    const uint32_t a = __builtin_bit_cast(uint32_t, x);
+    const auto r = __builtin_amdgcn_permlane32_swap(a, a, false, false);
+    const uint32_t lo = r[0], hi = r[1];
+    return f(__builtin_bit_cast(float, lo), __builtin_bit_cast(float, hi));
+}
+
+// Unpacks the pages of a batch's sequences, laid end to end, to bf16 pages
+// [page][kv head][16][128] and writes the table that names them.  One wave to a
+// (page, kv head).
+struct ChunkLengths {
+    const int32_t *indptr, *prefix;
+    int batch, bt_stride;
+    __device__ __forceinline__ int pages(int b) const {
+        if (b >= batch) return 0;
+        const int64_t len = static_cast<int64_t>(indptr[b + 1]) - indptr[b] + prefix[b];
+        const int64_t np = (len + kPageSize - 1) / kPageSize;
+        return static_cast<int>(max(int64_t{0}, min(np, static_cast<int64_t>(bt_stride))));
+    }
+};
+
+__global__ void __launch_bounds__(256)
+k_kv4_unpack(const uint8_t *__restrict__ kpool, const uint8_t *__restrict__ vpool, const uint8_t *__restrict__ scales,
+             uint16_t *__restrict__ kout, uint16_t *__restrict__ vout, int32_t *__restrict__ table, int table_stride,
+             const int32_t *__restrict__ indptr, const int32_t *__restrict__ prefix, const int32_t *__restrict__ bt,
+             int bt_stride, int batch, int num_pages, int hkv, int64_t items) {
+    const int lane = threadIdx.x & 63;
+    const int64_t item = static_cast<int64_t>(blockIdx.x) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if (item >= items) return;
+    const int page_no = static_cast<int>(item / hkv), h = static_cast<int>(item - static_cast<int64_t>(page_no) * hkv);
+    const ChunkLengths len{indptr, prefix, batch, bt_stride};
+    int running = 0, b = -1, p = 0;
+    for (int b0 = 0; b0 < batch; b0 += 64) {
+        const int np = len.pages(b0 + lane);
+        const int incl = running + lane_scan(np);
+        const uint64_t hit = __builtin_amdgcn_ballot_w64(page_no >= incl - np && page_no < incl);
+        if (hit) {
+            const int src = __builtin_ctzll(hit);
+            b = b0 + src;
+            p = page_no - __builtin_amdgcn_readlane(incl - np, src);
+            break;
+        }
+        running = __builtin_amdgcn_readlane(incl, 63);
+    }
+    if (b < 0 || p >= table_stride) return;  // device lengths that disagree with the host's
+    const int page = bt[static_cast<size_t>(b) * bt_stride + p];
+    const bool ok = page >= 0 && page < num_pages;
+    if (h == 0 && lane == 0) table[static_cast<size_t>(b) * table_stride + p] = ok ? page_no : -1;
+    if (!ok) return;
+    const size_t at = static_cast<size_t>(page) * hkv + h;
+    const uint8_t *sc = scales + at * kScaleBytes;
+    // K: four lane-contiguous dwords (8 dims) of codes, 16 bytes out each
+    const uint32_t *kc = reinterpret_cast<const uint32_t *>(kpool + at * kCodeBytes) + lane;
+    uint32_t codes_k[4], byte_k[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        codes_k[i] = kc[64 * i];
+        byte_k[i] = sc[((lane & 15) >> 2) * kPageSize + 4 * i + (lane >> 4)];
+    }
+    const int g = lane >> 4, c = lane & 15;
+    const uint4 vc = *reinterpret_cast<const uint4 *>(vpool + at * kCodeBytes + lane * 16);
+    uint32_t bytes[kBlocks], vr[4][kBlocks];
+#pragma unroll
+    for (int k = 0; k < kBlocks; ++k) bytes[k] = *reinterpret_cast<const uint32_t *>(sc + (kBlocks + k) * kPageSize + 4 * g);
+    uint4 *ko = reinterpret_cast<uint4 *>(kout + static_cast<size_t>(item) * (kPageSize * kHeadDim)) + lane;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) ko[64 * i] = decode_k(codes_k[i], byte_k[i]);
+    const uint32_t codes[kBlocks] = {vc.x, vc.y, vc.z, vc.w};
+    decode_v(codes, bytes, vr);
+    uint32_t *vo = reinterpret_cast<uint32_t *>(vout + static_cast<size_t>(item) * (kPageSize * kHeadDim)) + c;
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+        for (int k = 0; k < kBlocks; ++k) vo[(4 * g + t) * (kHeadDim / 2) + 16 * k] = vr[t][k];
+}
+
+// Workspace of a prefill call: K pages, V pages, their table, then the
+// workspace of the attention itself.
+struct UnpackLayout {
+    int64_t pages;
+    int64_t table_stride;
+    size_t off_v, off_table, off_ws;
+};
+mw_status unpack_layout(int32_t batch, const int32_t *h_new_lens, const int32_t *h_prefix_lens, int64_t hkv,
+                        UnpackLayout *u, const char *who) {
+    u->pages = 0;
+    u->table_stride = 1;
+    for (int32_t b = 0; b < batch; ++b) {
+        const int64_t np = (static_cast<int64_t>(h_new_lens[b]) + h_prefix_lens[b] + kPageSize - 1) / kPageSize;
+        u->pages += np;
+        u->table_stride = np > u->table_stride ? np : u->table_stride;
+    }
+    if (u->pages > INT32_MAX || u->pages * hkv > static_cast<int64_t>(INT32_MAX) * 4)
+        return fail(MW_ERR_UNSUPPORTED, "%s: too many pages", who);
+    const size_t pages_bytes = static_cast<size_t>(u->pages) * hkv * (kPageSize * kHeadDim * 2);
+    u->off_v = pages_bytes;
+    u->off_table = 2 * pages_bytes;
+    u->off_ws = (u->off_table + static_cast<size_t>(batch) * u->table_stride * 4 + 255) & ~static_cast<size_t>(255);
+    return MW_OK;
+}
+
+// ------------------------------------------------------- few rows: straight from the codes
+// A chunk of few rows reads each page for few query blocks, so unpacking it to
+// bf16 first (write 8192 bytes, read them again) costs more than it saves: 64
+// tokens over 8000 of 32/8 heads take 26 us like this and 37 unpacked, 16 tokens 18
+// and 34.  A tile takes 1.5 us of a CU with one work-group, 1.1 of each of two; it
+// is bound by the instructions that its four waves issue, not by memory (reading
+// the same tile over and over changes nothing; without the conversions it is 15-20%
+// shorter, without the exponentials or half of the second product 10% each).
+//
+// A work-group is four waves on 128 rows of a (sequence, kv head) (row = position *
+// group + head, 32 per wave) and one piece of their keys, 64 at a time:
+//   * S^T[key][row] = K Q^T on the scaled 32x32x64 instruction, K from memory as it
+//     lies (16 bytes a lane: one block of one key), Q as two e4m3 operands.
+//   * V is converted once for the four waves, a page each, into LDS in the order in
+//     which the second product takes it, [dim block][16 keys][half][dim][8 keys]:
+//     a lane of the page has four consecutive keys of eight dims, and the product's
+//     k slots of half h are keys 4h .. 4h+3 and 8+4h .. +3 of the 16, as the score
+//     registers hold them, so each dim is one 8-byte store and each operand one
+//     conflict-free 16-byte read.
+//   * the causal mask by position; online softmax as in the other kernels.
+// K of the next tile and the V codes of the one after it are on their way while a
+// tile is worked on; one barrier a tile.  A piece leaves (m, l) and its unnormalised
+// output in the workspace and k_kv4_merge adds them up, unless it is the only one.
+//
+// A value that a row does not see never reaches it through the scores; in the tile
+// of its own position a V block that is not finite does reach the rows before it
+// (0 times NaN), as in the bf16 kernels.
+constexpr int kBlockRows = 128;
+constexpr int kTileKeys = 64;
+constexpr int kMaxPieces = 64;  // (a lane of the merging wave each)
+constexpr int kTableTiles = 512;  // tiles of a piece, whose table entries fit the LDS copy
+
+struct FewRows {
+    float *o;      // [pieces][rows][hq][128]
+    float2 *ml;    // [pieces][rows][hq]
+    int64_t rows;  // of the call
+    int piece_tiles, max_pieces;
+};
+
+// A barrier for what the waves leave each other in LDS.  (__syncthreads would also
+// wait for the global loads on their way: 1.5 us a tile, whatever else it does.)
+__device__ __forceinline__ void tile_barrier() {
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+
+__global__ void __launch_bounds__(256, 2)
+k_kv4_prefill(const uint8_t *__restrict__ kpool, const uint8_t *__restrict__ vpool, const uint8_t *__restrict__ scales,
+              const uint16_t *__restrict__ q, uint16_t *__restrict__ out, const int32_t *__restrict__ indptr,
+              const int32_t *__restrict__ prefix, const int32_t *__restrict__ bt, int bt_stride, Divisor hkv, Divisor group,
+              Divisor blocks, int num_pages, float scale_log2, FewRows ws) {
+    __shared__ __attribute__((aligned(16))) char s_v[2][kTileKeys * kHeadDim * 2];
+    __shared__ __attribute__((aligned(16))) int32_t s_bt[4 * kTableTiles];  // (page, kv head) blocks; -1: absent
+    __shared__ int s_absent;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int l32 = lane & 31, half = lane >> 5;
+    // kv heads fastest: a die's L2 then has those of one
+    const int x = blockIdx.x, xb = x / hkv, kvh = x - xb * hkv, piece = xb / blocks, blk = xb - piece * blocks;
+    const int b = blockIdx.y;
+    const int row0 = indptr[b], n = indptr[b + 1] - row0, r = prefix[b];
+    const int rows = n * group, hq = hkv * group;
+    if (blk * kBlockRows >= rows || r < 0) return;
+    const int nt = prefill_block_tiles<int>(r, n, blk, kBlockRows, group);
+    const int pieces = prefill_pieces(nt, ws.piece_tiles, ws.max_pieces);
+    if (piece >= pieces) return;
+    const int t_lo = piece * nt / pieces, t_hi = (piece + 1) * nt / pieces;
+    if (t_hi - t_lo > kTableTiles) return;  // device lengths that disagree with the host's
+    const int len = r + n, np = min((len + kPageSize - 1) / kPageSize, bt_stride);
+    const int32_t *btrow = bt + static_cast<size_t>(b) * bt_stride;
+    if (threadIdx.x == 0) s_absent = 0;
+    __syncthreads();
+    for (int i = threadIdx.x; i < 4 * (t_hi - t_lo); i += 256) {
+        const int p = 4 * t_lo + i;
+        const int page = p < np ? btrow[p] : -1;
+        const bool there = page >= 0 && page < num_pages;
+        s_bt[i] = there ? page * hkv + kvh : -1;
+        if (!there) s_absent = 1;
+    }
+
+    // this lane's row, and the tiles that some row of the wave sees
+    const int first = blk * kBlockRows + 32 * wave;
+    const int mine = first + l32;
+    const bool valid = mine < rows;
+    const int pos = valid ? mine / group : n - 1, head = valid ? mine - pos * group : 0;
+    const int seen = r + pos;  // the last key it sees
+    const int nt_w = first < rows ? (r + min(first + 31, rows - 1) / group) / kTileKeys + 1 : 0;
+    i32x8 q_hi[2], q_lo[2];
+    float q_scale;
+    {
+        const uint16_t *qp = q + (static_cast<size_t>(row0 + pos) * hq + kvh * group + head) * kHeadDim + 16 * half;
+        uint4 raw[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            raw[i] = first < rows ? *reinterpret_cast<const uint4 *>(qp + 64 * (i >> 2) + 32 * (i >> 1 & 1) + 8 * (i & 1))
+                                  : make_uint4(0, 0, 0, 0);
+        const float f = split_q<false>(raw, q_hi, q_lo) * scale_log2;
+        q_scale = f < 1e-37f ? 1e-37f : f;  // (above 0, or a masked score would be a NaN; of a NaN row, NaN)
+    }
+    f32x16 oacc[4];
+#pragma unroll
+    for (int d = 0; d < 4; ++d) oacc[d] = f32x16{};
+    // a row may see no key of the piece's first tiles
+    float m_run = -__FLT_MAX__, l_run = 0.f;
+
+    // the lane's codes of a tile: K of keys l32 and 32 + l32, blocks half and 2 + half;
+    // V of page `wave`, key quad g, dims 32 b + 2 c, + 1
+    const int g = lane >> 4, c = lane & 15;
+    uint4 kc[4], vc = make_uint4(0, 0, 0, 0);
+    uint32_t ks[4], vs[kBlocks] = {0, 0, 0, 0};
+    const uint8_t *const k_lane = kpool + (l32 & 15) * 64 + half * 16;
+    const uint8_t *const ks_lane = scales + half * kPageSize + (l32 & 15);
+    const auto load_k = [&](int t) __attribute__((always_inline)) {
+        const int32_t *at = s_bt + 4 * (t - t_lo);
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) {
+            const size_t block = max(at[2 * kb + (l32 >> 4)], 0);
+            const uint8_t *src = k_lane + block * kCodeBytes, *sc = ks_lane + block * kScaleBytes;
+#pragma unroll
+            for (int d = 0; d < 2; ++d) {
+                kc[2 * kb + d] = *reinterpret_cast<const uint4 *>(src + 32 * d);
+                ks[2 * kb + d] = sc[2 * kPageSize * d];
+            }
+        }
+    };
+    const auto load_v = [&](int t) __attribute__((always_inline)) {
+        const size_t block = max(__builtin_amdgcn_readfirstlane(s_bt[4 * (t - t_lo) + wave]), 0);
+        vc = *reinterpret_cast<const uint4 *>(vpool + block * kCodeBytes + lane * 16);
+        const uint8_t *sc = scales + block * kScaleBytes + kBlocks * kPageSize + 4 * g;
+#pragma unroll
+        for (int i = 0; i < kBlocks; ++i) vs[i] = *reinterpret_cast<const uint32_t *>(sc + i * kPageSize);
+    };
+    const auto store_v = [&](int t, char *buf) __attribute__((always_inline)) {
+        // keys past the sequence or on an absent page are zeros: 0 times the infinite
+        // scale of a slack slot would not be 0
+        const int there = __builtin_amdgcn_readfirstlane(s_bt[4 * (t - t_lo) + wave]) < 0 ? 0 : len - (t * kTileKeys + wave * kPageSize + 4 * g);
+        const uint32_t mask = there >= 4 ? ~0u : there <= 0 ? 0u : (1u << 8 * there) - 1;
+        const uint32_t codes[kBlocks] = {vc.x, vc.y, vc.z, vc.w};
+        uint32_t bytes[kBlocks], v[4][kBlocks];
+#pragma unroll
+        for (int i = 0; i < kBlocks; ++i) bytes[i] = vs[i] & mask;
+        decode_v(codes, bytes, v);
+        char *dst = buf + (2 * wave + (g & 1)) * 512 + c * 32 + (g >> 1) * 8;
+#pragma unroll
+        for (int i = 0; i < kBlocks; ++i) {
+            // two dims of four keys each to four keys of two dims
+            *reinterpret_cast<uint2 *>(dst + i * 4096) =
+                make_uint2(__builtin_amdgcn_perm(v[1][i], v[0][i], 0x05040100), __builtin_amdgcn_perm(v[3][i], v[2][i], 0x05040100));
+            *reinterpret_cast<uint2 *>(dst + i * 4096 + 16) =
+                make_uint2(__builtin_amdgcn_perm(v[1][i], v[0][i], 0x07060302), __builtin_amdgcn_perm(v[3][i], v[2][i], 0x07060302));
+        }
+    };
+
+    // (the last tile's loads are made again instead of none: with loads that may not
+    // have been made the compiler waits for all that may be on their way)
+    const int t_end = t_hi - 1;
+    __syncthreads();
+    const bool absent = s_absent != 0;
+    load_v(t_lo);
+    load_k(t_lo);
+    store_v(t_lo, s_v[0]);
+    load_v(min(t_lo + 1, t_end));
+    tile_barrier();
+    int t = t_lo;
+    for (const int t_seen = min(t_hi, nt_w); t < t_seen; ++t) {
+        // the matrix instructions of the scores, with the conversion of the next tile's
+        // V between them
+        f32x16 sc[2];
+        {
+            if (absent) {  // keys on an absent page are zeros
+                const int32_t *at = s_bt + 4 * (t - t_lo);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const bool there = at[2 * (i >> 1) + (l32 >> 4)] >= 0;
+                    kc[i] = sel4(there, kc[i]);
+                    ks[i] = there ? ks[i] : kBias;
+                }
+            }
+            const f32x16 zero{};
+#pragma unroll
+            for (int d = 0; d < 2; ++d)
+#pragma unroll
+                for (int part = 0; part < 2; ++part)
+#pragma unroll
+                    for (int kb = 0; kb < 2; ++kb) {
+                        const uint4 k = kc[2 * kb + d];
+                        const i32x8 a{static_cast<int>(k.x), static_cast<int>(k.y), static_cast<int>(k.z), static_cast<int>(k.w), 0, 0, 0, 0};
+                        const int sb = static_cast<int>(ks[2 * kb + d]);
+                        sc[kb] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, part ? q_lo[d] : q_hi[d], d + part ? sc[kb] : zero,
+                                                                                 4, 0, 0, sb, 0, 127);
+                    }
+        }
+        // the loads below go to the registers that the instructions above have read: moved
+        // up they would take others, to be waited for and copied at the end of the tile
+        __builtin_amdgcn_sched_barrier(0);
+        load_k(min(t + 1, t_end));
+        store_v(min(t + 1, t_end), s_v[(t + 1 - t_lo) & 1]);
+        __builtin_amdgcn_sched_barrier(0);
+        load_v(min(t + 2, t_end));
+        {
+            const int k0 = t * kTileKeys;
+            if (k0 + kTileKeys - 1 > r + first / group) {  // some row of the wave does not see the whole tile
+#pragma unroll
+                for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        if (k0 + 32 * kb + 8 * (i >> 2) + 4 * half + (i & 3) > seen) sc[kb][i] = -INFINITY;
+            }
+            float mx = -INFINITY;
+#pragma unroll
+            for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                for (int i = 0; i < 16; i += 2)
+                    mx = __builtin_elementwise_maximum(__builtin_elementwise_maximum(mx, sc[kb][i]), sc[kb][i + 1]);
+            mx = across_half(mx, [](float a, float b) { return __builtin_elementwise_maximum(a, b); }) * q_scale;
+            if (__builtin_amdgcn_ballot_w64(mx > m_run + kRescaleLog2) != 0) {
+                const float m_new = fmaxf(m_run, mx);
+                const float alpha = __builtin_amdgcn_exp2f(m_run - m_new);
+                m_run = m_new;
+                l_run *= alpha;
+#pragma unroll
+                for (int d = 0; d < 4; ++d) oacc[d] *= alpha;
+            }
+            bf16x8 p[4];
+#pragma unroll
+            for (int s = 0; s < 4; ++s) {
+                float w[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    w[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[s >> 1][8 * (s & 1) + i], q_scale, -m_run));
+                l_run += ((w[0] + w[1]) + (w[2] + w[3])) + ((w[4] + w[5]) + (w[6] + w[7]));
+                p[s] = __builtin_bit_cast(bf16x8, make_uint4(cvt2(w[0], w[1]), cvt2(w[2], w[3]), cvt2(w[4], w[5]), cvt2(w[6], w[7])));
+            }
+            const char *vb = s_v[(t - t_lo) & 1] + half * 512 + l32 * 16;
+#pragma unroll
+            for (int s = 0; s < 4; ++s)
+#pragma unroll
+                for (int d = 0; d < 4; ++d)
+                    oacc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+                        *reinterpret_cast<const bf16x8 *>(vb + (4 * d + s) * 1024), p[s], oacc[d], 0, 0, 0);
+        }
+        tile_barrier();
+    }
+    for (; t < t_hi; ++t) {  // tiles past all of the wave's rows: its page of each only
+        store_v(min(t + 1, t_end), s_v[(t + 1 - t_lo) & 1]);
+        load_v(min(t + 2, t_end));
+        tile_barrier();
+    }
+    if (!valid) return;
+    l_run = across_half(l_run, [](float a, float b) { return a + b; });
+    const size_t at = static_cast<size_t>(row0 + pos) * hq + kvh * group + head;
+    if (pieces == 1) {
+        const float inv = 1.f / l_run;
+#pragma unroll
+        for (int d = 0; d < 4; ++d)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                *reinterpret_cast<uint2 *>(out + at * kHeadDim + 32 * d + 8 * i + 4 * half) =
+                    make_uint2(cvt2(oacc[d][4 * i] * inv, oacc[d][4 * i + 1] * inv),
+                               cvt2(oacc[d][4 * i + 2] * inv, oacc[d][4 * i + 3] * inv));
+        return;
+    }
+    const size_t slot = static_cast<size_t>(piece) * ws.rows * hq + at;
+#pragma unroll
+    for (int d = 0; d < 4; ++d)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            *reinterpret_cast<f32x4 *>(ws.o + slot * kHeadDim + 32 * d + 8 * i + 4 * half) =
+                f32x4{oacc[d][4 * i], oacc[d][4 * i + 1], oacc[d][4 * i + 2], oacc[d][4 * i + 3]};
+    if (half == 0) ws.ml[slot] = make_float2(m_run, l_run);
+}
+
+// The pieces of every row that has more than one, a wave to a (row, head).
+__global__ void __launch_bounds__(256)
+k_kv4_merge(uint16_t *__restrict__ out, const int32_t *__restrict__ indptr, const int32_t *__restrict__ prefix, Divisor hq,
+            Divisor group, FewRows ws) {
+    const int b = blockIdx.y, row0 = indptr[b], n = indptr[b + 1] - row0;
+    const int lane = threadIdx.x & 63, at = 4 * blockIdx.x + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int i = at / hq, h = at - i * hq;
+    if (i >= n) return;
+    const int nt = prefill_block_tiles<int>(prefix[b], n, (i * group + (h - h / group * group)) / kBlockRows, kBlockRows, group);
+    const int pieces = prefill_pieces(nt, ws.piece_tiles, ws.max_pieces);
+    if (pieces < 2) return;
+    const size_t slot = static_cast<size_t>(row0 + i) * hq + h, step = static_cast<size_t>(ws.rows) * hq;
+    HeadSum s;
+    s.add(ws.ml[min(lane, pieces - 1) * step + slot], pieces, lane, [&](int p) __attribute__((always_inline)) {
+        return reinterpret_cast<const float2 *>(ws.o + (p * step + slot) * kHeadDim)[lane];
+    });
+    const float inv = 1.f / s.L;
+    reinterpret_cast<uint32_t *>(out + slot * kHeadDim)[lane] = cvt2(s.acc.x * inv, s.acc.y * inv);
+}
+
+// Whether a call goes straight from the codes, and in which pieces.  By the costs
+// below, fitted to 28 calls of 1 to 500 tokens over 0 to 30000 made all three ways
+// (within 27% of each, most within 10%): straight from the codes with one
+// work-group to a CU or with two that slow each other down, or unpacked first.  One
+// sequence, 8 kv heads of 4 query heads, us (one, two, unpacked):
+//     64 tokens over 2000     18.8   23   22        64 over 8000    28    32   37.5
+//     64 over 30000           63     59   84.6     256 over 8000    66    63   56
+//     16 sequences of 32 over 4000   71    67  118
+// The costs are those of a whole MI355X whatever CUs the stream has, so that the
+// workspace and the results do not depend on it; both ways slow down alike.
+constexpr int kCus = 256;
+constexpr int kFewBlocks = 8;  // (unpacked pages read by more blocks have paid for themselves)
+struct FewCost {
+    double fixed, tile, byte;  // us of a call, of a tile of the longest piece, of a byte of partials
+};
+constexpr FewCost kFewCost[2] = {{7.0, 1.6, 0.24e-6}, {10.5, 2.25, 0.21e-6}};
+constexpr FewCost kUnpackCost = {16.5, 0.85, 0.233e-6};  // of a call, of a tile per CU, of a byte of pages
+struct FewPlan {
+    bool use;        // straight from the codes
+    int64_t blocks;  // most query blocks of a (sequence, kv head)
+    int piece_tiles, max_pieces;
+    size_t bytes;    // of workspace
+};
+FewPlan few_plan(int32_t batch, const int32_t *h_new_lens, const int32_t *h_prefix_lens, int64_t hkv, int64_t group) {
+    FewPlan p{};
+    int64_t rows = 0, tiles = 0, work = 0, most = 0;
+    const auto blocks_of = [&](int32_t b) { return (h_new_lens[b] * group + kBlockRows - 1) / kBlockRows; };
+    const auto tiles_of = [&](int32_t b) {
+        return h_new_lens[b] == 0 ? 0 : (static_cast<int64_t>(h_prefix_lens[b]) + h_new_lens[b] + kTileKeys - 1) / kTileKeys;
+    };
+    for (int32_t b = 0; b < batch; ++b) {
+        rows += h_new_lens[b];
+        tiles += tiles_of(b);
+        work += blocks_of(b) * tiles_of(b);
+        p.blocks = std::max(p.blocks, blocks_of(b));
+        most = std::max(most, tiles_of(b));
+    }
+    if (rows == 0 || p.blocks > kFewBlocks || most > static_cast<int64_t>(kTableTiles) * kMaxPieces) return p;
+    const double tile_bytes = kTileKeys * kHeadDim * 4 + kTileKeys / kPageSize * (2 * kCodeBytes + kScaleBytes);
+    double best = kUnpackCost.fixed + kUnpackCost.tile * static_cast<double>(work * hkv) / kCus +
+                  kUnpackCost.byte * tile_bytes * static_cast<double>(tiles * hkv);
+    for (int per_cu = 1; per_cu <= 2; ++per_cu) {
+        const int64_t slots = per_cu * kCus;
+        const auto groups = [&](int64_t len) {
+            int64_t sum = 0;
+            for (int32_t b = 0; b < batch; ++b) sum += blocks_of(b) * ((tiles_of(b) + len - 1) / len);
+            return sum * hkv;
+        };
+        // the shortest pieces that all run at once, as far as there are such
+        int64_t lo = std::max<int64_t>(2, (most + kMaxPieces - 1) / kMaxPieces);
+        for (int64_t hi = std::max(lo, std::min<int64_t>(most, kTableTiles)); lo < hi;) {
+            const int64_t mid = (lo + hi) / 2;
+            if (groups(mid) <= slots)
+                hi = mid;
+            else
+                lo = mid + 1;
+        }
+        const int64_t pieces = (most + lo - 1) / lo, rounds = (groups(lo) + slots - 1) / slots;
+        const size_t bytes = pieces > 1 ? static_cast<size_t>(pieces) * rows * hkv * group * (kHeadDim * 4 + 8) : 0;
+        const FewCost &c = kFewCost[per_cu - 1];
+        const double us = c.fixed + c.tile * static_cast<double>(std::min(lo, most) * rounds) + c.byte * 2.0 * static_cast<double>(bytes);
+        if (us >= best) continue;
+        best = us;
+        p.use = true;
+        p.piece_tiles = static_cast<int>(lo);
+        p.max_pieces = static_cast<int>(pieces);
+        p.bytes = bytes;
+    }
+    return p;
+}
+
+}  // namespace
+
+extern "C" {
+
+mw_status mw_kv4_prefill_workspace_size(const mw_attn_shape *shape, int32_t batch, const int32_t *h_new_lens,
+                                        const int32_t *h_prefix_lens, int32_t num_cus, size_t *bytes) {
+    const char *who = "mw_kv4_prefill_workspace_size";
+    size_t inner = 0;
+    mw_status st = mw_prefill_workspace_size(shape, batch, h_new_lens, h_prefix_lens, num_cus, &inner);
+    if (st != MW_OK) return st;
+    if (!bytes) return fail(MW_ERR_INVALID_ARG, "%s: bytes is NULL", who);
+    const FewPlan few = few_plan(batch, h_new_lens, h_prefix_lens, shape->num_kv_heads, shape->num_q_heads / shape->num_kv_heads);
+    if (few.use) {
+        *bytes = few.bytes;
+        return MW_OK;
+    }
+    UnpackLayout u;
+    st = unpack_layout(batch, h_new_lens, h_prefix_lens, shape->num_kv_heads, &u, who);
+    if (st != MW_OK) return st;
+    *bytes = u.off_ws + inner;
+    return MW_OK;
+}
+
+mw_status mw_kv4_prefill_attn(const mw_kv_pool *pool, const mw_attn_shape *shape, int32_t batch,
+                              const int32_t *h_new_lens, const int32_t *h_prefix_lens, const int32_t *d_qo_indptr,
+                              const int32_t *d_prefix_lens, const int32_t *d_block_table, int32_t bt_stride,
+                              const void *d_q, void *d_out, void *d_workspace, size_t workspace_bytes, mw_stream stream,
+                              mw_timing *timing) {
+    const char *who = "mw_kv4_prefill_attn";
+    int64_t max_n = 0, total = 0;
+    mw_status st = check_rows(pool, batch, h_new_lens, h_prefix_lens, d_qo_indptr, d_prefix_lens, d_block_table,
+                              bt_stride, &max_n, &total, who);
+    if (st == MW_OK) st = check_pool_kind(pool, true, who);
+    if (st == MW_OK && !shape) st = fail(MW_ERR_INVALID_ARG, "%s: bad arguments", who);
+    if (st != MW_OK) return st;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    const int64_t cus = stream_cus(s);
+    // every check of the attention call: on a bf16 pool in the place of this one
+    mw_kv_pool bf16{};
+    bf16.desc = pool->desc;
+    mw_prefill_args a{&bf16,         *shape,        batch,         h_new_lens, h_prefix_lens, d_qo_indptr,
+                      d_prefix_lens, d_block_table, bt_stride,     d_q,        d_out};
+    PrefillPlan pl;
+    st = prefill_prepare(&a, cus, true, &pl, who, true);
+    if (st != MW_OK) return st;
+    const FewPlan few = few_plan(batch, h_new_lens, h_prefix_lens, pl.hkv, pl.group);
+    if (total == 0) {
+        st = timing_begin(timing, s);
+        if (st == MW_OK) st = timing_kernel_done(timing, s);
+        timing_end(timing);
+        return st;
+    }
+    if (few.use) {
+        if (workspace_bytes < few.bytes || (few.bytes > 0 && (!d_workspace || !aligned16(d_workspace))))
+            return fail(MW_ERR_INVALID_ARG, "%s: needs a 16-byte aligned workspace of %zu bytes (got %zu)", who, few.bytes,
+                        workspace_bytes);
+        float *ws = static_cast<float *>(d_workspace);
+        const size_t values = static_cast<size_t>(few.max_pieces) * total * shape->num_q_heads;
+        const FewRows rows{ws, reinterpret_cast<float2 *>(ws + values * kHeadDim), total, few.piece_tiles, few.max_pieces};
+        st = timing_begin(timing, s);
+        if (st != MW_OK) return st;
+        hipLaunchKernelGGL(k_kv4_prefill, dim3(static_cast<unsigned>(few.blocks * pl.hkv * few.max_pieces), batch), dim3(256), 0,
+                           s, pool->k4, pool->v4, pool->scales, static_cast<const uint16_t *>(d_q),
+                           static_cast<uint16_t *>(d_out), d_qo_indptr, d_prefix_lens, d_block_table, bt_stride,
+                           Divisor(pl.hkv), Divisor(pl.group), Divisor(static_cast<int>(few.blocks)), pool->desc.num_pages,
+                           pl.scale_log2, rows);
+        st = check_launch("k_kv4_prefill");
+        if (st == MW_OK) st = timing_kernel_done(timing, s);
+        if (st == MW_OK && few.max_pieces > 1) {
+            hipLaunchKernelGGL(k_kv4_merge, dim3(static_cast<unsigned>((max_n * shape->num_q_heads + 3) / 4), batch), dim3(256), 0,
+                               s, static_cast<uint16_t *>(d_out), d_qo_indptr, d_prefix_lens, Divisor(shape->num_q_heads),
+                               Divisor(pl.group), rows);
+            st = check_launch("k_kv4_merge");
+            if (st == MW_OK) st = timing_kernel_done(timing, s);
+        }
+        timing_end(timing);
+        return st;
+    }
+    UnpackLayout u;
+    st = unpack_layout(batch, h_new_lens, h_prefix_lens, pl.hkv, &u, who);
+    if (st != MW_OK) return st;
+    if (!d_workspace || !aligned16(d_workspace) || workspace_bytes < u.off_ws)
+        return fail(MW_ERR_INVALID_ARG, "%s: needs a 16-byte aligned workspace of %zu bytes and the attention's (got %zu)",
+                    who, u.off_ws, workspace_bytes);
+    char *ws = static_cast<char *>(d_workspace);
+    // the unpacked pages are the pool that the attention reads
+    bf16.desc.num_pages = static_cast<int32_t>(u.pages);
+    bf16.k = reinterpret_cast<uint16_t *>(ws);
+    bf16.v = reinterpret_cast<uint16_t *>(ws + u.off_v);
+    int32_t *table = reinterpret_cast<int32_t *>(ws + u.off_table);
+    a.d_block_table = table;
+    a.bt_stride = static_cast<int32_t>(u.table_stride);
+    a.d_workspace = ws + u.off_ws;
+    a.workspace_bytes = workspace_bytes - u.off_ws;
+    st = prefill_fit_workspace(&a, cus, &pl, a.d_workspace, a.workspace_bytes, who);
+    if (st == MW_OK) st = timing_begin(timing, s);
+    if (st != MW_OK) return st;
+    const int64_t items = u.pages * pool->desc.num_kv_heads;
+    hipLaunchKernelGGL(k_kv4_unpack, dim3(static_cast<unsigned>((items + 3) / 4)), dim3(256), 0, s, pool->k4, pool->v4,
+                       pool->scales, bf16.k, bf16.v, table, static_cast<int>(u.table_stride), d_qo_indptr, d_prefix_lens,
+                       d_block_table, bt_stride, batch, pool->desc.num_pages, pool->desc.num_kv_heads, items);
+    st = check_launch("k_kv4_unpack");
+    if (st == MW_OK) st = timing_kernel_done(timing, s);
+    if (st != MW_OK) return st;
+    return prefill_launch(a, pl, s, timing);
+}
+
+}  // extern "C"

@@ -20,7 +20,8 @@ BORDERS = ((0.25, False), (0.75, True), (1.25, False), (1.75, True), (2.5, False
 
 def quantise(bits):
     """bf16 bits [..., 128] -> (codes uint8 [..., 128], scale bytes uint8 [..., 4])."""
-    x = bits_to_f32(bits).astype(np.float64).reshape(*bits.shape[:-1], BLOCKS, 32)
+    with np.errstate(invalid="ignore"):  # (signalling NaNs)
+        x = bits_to_f32(bits).astype(np.float64).reshape(*bits.shape[:-1], BLOCKS, 32)
     finite = np.isfinite(x).all(-1)
     most = np.abs(np.where(finite[..., None], x, 0)).max(-1)
     with np.errstate(divide="ignore"):

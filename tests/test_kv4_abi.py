@@ -111,21 +111,30 @@ def test_decode(pool4):
 
 
 def test_prefill(pool4):
-    new, prefix = [20, 3], [0, 40]
+    # a chunk of many rows is unpacked: pages of two heads and a table of two rows
+    new, prefix = [1000, 3], [0, 40]
     size = mw.mw_kv4_prefill_workspace_size(4, 2, 128, new, prefix)
-    assert size >= 2 * 5 * 2 * 4096 + 2 * 3 * 4   # five pages of two heads, a table of two rows
+    assert size >= 2 * 66 * 2 * 4096 + 2 * 63 * 4
+    # of few rows over few keys it needs nothing, over many its pieces' sums
+    few = mw.mw_kv4_prefill_workspace_size(4, 2, 128, [20, 3], [4000, 40])
+    assert mw.mw_kv4_prefill_workspace_size(4, 2, 128, [20, 3], [0, 40]) == 0
+    assert few > 0 and few % (23 * 4 * 520) == 0
+    for cus in (0, 32, 256):
+        assert mw.mw_kv4_prefill_workspace_size(4, 2, 128, [20, 3], [4000, 40], cus) == few
     # long lengths are sized in 64 bits
     far = mw.mw_kv4_prefill_workspace_size(64, 8, 128, [4096] * 64, [100000] * 64)
     assert far >= 2 * 64 * ((104096 + 15) // 16) * 8 * 4096 > 1 << 32
 
-    def call(hq=4, hkv=2, d=128, scale=0.1, new=new, prefix=prefix, ip=0x100, pl=0x200, bt=0x300, stride=3, q=0x400,
+    def call(hq=4, hkv=2, d=128, scale=0.1, new=new, prefix=prefix, ip=0x100, pl=0x200, bt=0x300, stride=500, q=0x400,
              out=0x500, ws=0x600, n=size):
         mw.mw_kv4_prefill_attn(pool4, hq, hkv, d, scale, new, prefix, ip, pl, bt, stride, q, out, ws, n)
 
-    for kw in (dict(new=[20, 9]), dict(new=[-1, 3]), dict(prefix=[-1, 40]), dict(scale=0.0), dict(hkv=4), dict(hq=3),
-               dict(ws=0), dict(ws=0x608), dict(n=2 * 5 * 2 * 4096), dict(q=0x408), dict(out=0), dict(ip=0),
-               dict(bt=0), dict(stride=0)):
-        refused(mw.MW_ERR_INVALID_ARG, call, **kw)
+    shapes = ((new, prefix, 2 * 66 * 2 * 4096), ([20, 3], [4000, 40], few - 1))
+    for new_, prefix_, short in shapes:
+        for kw in (dict(new=[20, 8000]), dict(new=[-1, 3]), dict(prefix=[-1, 40]), dict(scale=0.0), dict(hkv=4),
+                   dict(hq=3), dict(ws=0), dict(ws=0x608), dict(n=short), dict(n=0), dict(q=0x408), dict(out=0),
+                   dict(ip=0), dict(bt=0), dict(stride=0), dict(stride=2)):
+            refused(mw.MW_ERR_INVALID_ARG, call, **(dict(new=new_, prefix=prefix_) | kw))
     refused(mw.MW_ERR_UNSUPPORTED, call, d=64)
     refused(mw.MW_ERR_INVALID_ARG, mw.mw_kv4_prefill_workspace_size, 4, 2, 128, [5], [-3])
     call(new=[0, 0], prefix=[0, 0], ws=0, n=0)    # nothing to do

@@ -147,11 +147,19 @@ constexpr int kTileKeys = 64;
 constexpr int kMaxPieces = 64;  // (a lane of the merging wave each)
 constexpr int kTableTiles = 512;  // tiles of a piece, whose table entries fit the LDS copy
 
+// The work-groups of a call: those of a sequence after the earlier ones', its pieces'
+// blocks in turn, kv heads fastest (a die's L2 then has those of one).  What a group
+// leaves stands at its number: rows of the largest block each.
 struct FewRows {
-    float *o;      // [pieces][rows][hq][128]
-    float2 *ml;    // [pieces][rows][hq]
-    int64_t rows;  // of the call
-    int piece_tiles, max_pieces;
+    float *o;    // [groups][block_rows][128]
+    float2 *ml;  // [groups][block_rows]
+    int groups, block_rows, piece_tiles, max_pieces;
+    // (blocks, pieces at most) of a sequence
+    __device__ __forceinline__ int2 of(int n, int r, int group) const {
+        if (n <= 0 || r < 0) return make_int2(0, 0);
+        const int tiles = (r + n + kTileKeys - 1) / kTileKeys;
+        return make_int2((n * group + kBlockRows - 1) / kBlockRows, prefill_pieces(tiles, piece_tiles, max_pieces));
+    }
 };
 
 // A barrier for what the waves leave each other in LDS.  (__syncthreads would also
@@ -165,24 +173,42 @@ __device__ __forceinline__ void tile_barrier() {
 __global__ void __launch_bounds__(256, 2)
 k_kv4_prefill(const uint8_t *__restrict__ kpool, const uint8_t *__restrict__ vpool, const uint8_t *__restrict__ scales,
               const uint16_t *__restrict__ q, uint16_t *__restrict__ out, const int32_t *__restrict__ indptr,
-              const int32_t *__restrict__ prefix, const int32_t *__restrict__ bt, int bt_stride, Divisor hkv, Divisor group,
-              Divisor blocks, int num_pages, float scale_log2, FewRows ws) {
+              const int32_t *__restrict__ prefix, const int32_t *__restrict__ bt, int bt_stride, int batch, Divisor hkv,
+              Divisor group, int num_pages, float scale_log2, FewRows ws) {
     __shared__ __attribute__((aligned(16))) char s_v[2][kTileKeys * kHeadDim * 2];
     __shared__ __attribute__((aligned(16))) int32_t s_bt[4 * kTableTiles];  // (page, kv head) blocks; -1: absent
     __shared__ int s_absent;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int l32 = lane & 31, half = lane >> 5;
-    // kv heads fastest: a die's L2 then has those of one
-    const int x = blockIdx.x, xb = x / hkv, kvh = x - xb * hkv, piece = xb / blocks, blk = xb - piece * blocks;
-    const int b = blockIdx.y;
-    const int row0 = indptr[b], n = indptr[b + 1] - row0, r = prefix[b];
+    // 64 sequences at a time are searched for this work-group's
+    const int x = blockIdx.x, xb = x / hkv, kvh = x - xb * hkv;
+    int b = -1, row0 = 0, n = 0, r = 0, nqb = 1, at_b = 0;
+    for (int b0 = 0, running = 0; b0 < batch; b0 += 64) {
+        const int at = min(b0 + lane, batch - 1), row = indptr[at], len = indptr[at + 1] - row, pre = prefix[at];
+        const int2 of = ws.of(b0 + lane < batch ? len : 0, pre, group);
+        const int count = of.x * of.y, incl = running + lane_scan(count);
+        const uint64_t hit = __builtin_amdgcn_ballot_w64(xb >= incl - count && xb < incl);
+        if (hit) {
+            const int src = __builtin_ctzll(hit);
+            b = b0 + src;
+            at_b = xb - __builtin_amdgcn_readlane(incl - count, src);
+            row0 = __builtin_amdgcn_readlane(row, src);
+            n = __builtin_amdgcn_readlane(len, src);
+            r = __builtin_amdgcn_readlane(pre, src);
+            nqb = __builtin_amdgcn_readlane(of.x, src);
+            break;
+        }
+        running = __builtin_amdgcn_readlane(incl, 63);
+    }
+    if (b < 0) return;
+    const int piece = at_b / nqb, blk = at_b - piece * nqb;
     const int rows = n * group, hq = hkv * group;
-    if (blk * kBlockRows >= rows || r < 0) return;
     const int nt = prefill_block_tiles<int>(r, n, blk, kBlockRows, group);
+    // (device lengths that disagree with the host's)
+    if (nt <= 0 || nt > ws.piece_tiles * ws.max_pieces || min(kBlockRows, rows - blk * kBlockRows) > ws.block_rows) return;
     const int pieces = prefill_pieces(nt, ws.piece_tiles, ws.max_pieces);
     if (piece >= pieces) return;
     const int t_lo = piece * nt / pieces, t_hi = (piece + 1) * nt / pieces;
-    if (t_hi - t_lo > kTableTiles) return;  // device lengths that disagree with the host's
     const int len = r + n, np = min((len + kPageSize - 1) / kPageSize, bt_stride);
     const int32_t *btrow = bt + static_cast<size_t>(b) * bt_stride;
     if (threadIdx.x == 0) s_absent = 0;
@@ -377,7 +403,7 @@ k_kv4_prefill(const uint8_t *__restrict__ kpool, const uint8_t *__restrict__ vpo
                                cvt2(oacc[d][4 * i + 2] * inv, oacc[d][4 * i + 3] * inv));
         return;
     }
-    const size_t slot = static_cast<size_t>(piece) * ws.rows * hq + at;
+    const size_t slot = static_cast<size_t>(x) * ws.block_rows + mine - blk * kBlockRows;
 #pragma unroll
     for (int d = 0; d < 4; ++d)
 #pragma unroll
@@ -389,91 +415,122 @@ k_kv4_prefill(const uint8_t *__restrict__ kpool, const uint8_t *__restrict__ vpo
 
 // The pieces of every row that has more than one, a wave to a (row, head).
 __global__ void __launch_bounds__(256)
-k_kv4_merge(uint16_t *__restrict__ out, const int32_t *__restrict__ indptr, const int32_t *__restrict__ prefix, Divisor hq,
+k_kv4_merge(uint16_t *__restrict__ out, const int32_t *__restrict__ indptr, const int32_t *__restrict__ prefix, Divisor hkv,
             Divisor group, FewRows ws) {
-    const int b = blockIdx.y, row0 = indptr[b], n = indptr[b + 1] - row0;
+    const int b = blockIdx.y, row0 = indptr[b], n = indptr[b + 1] - row0, r = prefix[b], hq = hkv * group;
     const int lane = threadIdx.x & 63, at = 4 * blockIdx.x + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int i = at / hq, h = at - i * hq;
-    if (i >= n) return;
-    const int nt = prefill_block_tiles<int>(prefix[b], n, (i * group + (h - h / group * group)) / kBlockRows, kBlockRows, group);
+    const int pos_kvh = at / group, pos = pos_kvh / hkv, kvh = pos_kvh - pos * hkv;
+    if (pos >= n) return;
+    const int row = pos * group + at - pos_kvh * group, blk = row / kBlockRows;
+    const int nt = prefill_block_tiles<int>(r, n, blk, kBlockRows, group);
     const int pieces = prefill_pieces(nt, ws.piece_tiles, ws.max_pieces);
     if (pieces < 2) return;
-    const size_t slot = static_cast<size_t>(row0 + i) * hq + h, step = static_cast<size_t>(ws.rows) * hq;
+    int first = blk;  // the work-group of the block's first piece, then over kv heads
+    for (int b0 = 0; b0 < b; b0 += 64) {
+        const int seq = min(b0 + lane, b);
+        const int2 of = ws.of(seq < b ? indptr[seq + 1] - indptr[seq] : 0, prefix[seq], group);
+        first += __builtin_amdgcn_readlane(lane_scan(of.x * of.y), 63);
+    }
+    first = first * hkv + kvh;
+    const int step = ws.of(n, r, group).x * hkv;
+    if (first < 0 || first + (pieces - 1) * step >= ws.groups) return;  // (device lengths that disagree with the host's)
+    const size_t slot = static_cast<size_t>(first) * ws.block_rows + row - blk * kBlockRows;
+    const size_t next = static_cast<size_t>(step) * ws.block_rows;
     HeadSum s;
-    s.add(ws.ml[min(lane, pieces - 1) * step + slot], pieces, lane, [&](int p) __attribute__((always_inline)) {
-        return reinterpret_cast<const float2 *>(ws.o + (p * step + slot) * kHeadDim)[lane];
+    s.add(ws.ml[slot + min(lane, pieces - 1) * next], pieces, lane, [&](int p) __attribute__((always_inline)) {
+        return reinterpret_cast<const float2 *>(ws.o + (slot + p * next) * kHeadDim)[lane];
     });
     const float inv = 1.f / s.L;
-    reinterpret_cast<uint32_t *>(out + slot * kHeadDim)[lane] = cvt2(s.acc.x * inv, s.acc.y * inv);
+    reinterpret_cast<uint32_t *>(out + (static_cast<size_t>(row0) * hq + at) * kHeadDim)[lane] = cvt2(s.acc.x * inv, s.acc.y * inv);
 }
 
-// Whether a call goes straight from the codes, and in which pieces.  By the costs
-// below, fitted to 28 calls of 1 to 500 tokens over 0 to 30000 made all three ways
-// (within 27% of each, most within 10%): straight from the codes with one
-// work-group to a CU or with two that slow each other down, or unpacked first.  One
-// sequence, 8 kv heads of 4 query heads, us (one, two, unpacked):
-//     64 tokens over 2000     18.8   23   22        64 over 8000    28    32   37.5
-//     64 over 30000           63     59   84.6     256 over 8000    66    63   56
-//     16 sequences of 32 over 4000   71    67  118
+// Whether a call goes straight from the codes, and in which pieces: by the costs
+// below, fitted to 82 calls of 1 to 500 tokens over 0 to 30000, of one sequence and
+// of batches, of 1 to 32 kv heads, each made all three ways: straight from the codes
+// with one work-group to a CU, with two that slow each other down, or unpacked
+// first.  The way so chosen took 1% longer than the fastest in the mean and 14% at
+// most.  us (one, two, unpacked), 8 kv heads of 4 query heads:
+//       1 token over 0           6.7    6.7   11.4      64 over 2000      18.5  22.2  22.6
+//      16 tokens over 8000      18.1   20.9   33.3      64 over 30000     64    58    86
+//     256 tokens over 0         16.1   15.8   12.9     256 over 8000      63    59    56
+//     16 sequences of 4 over 4000  51  37    112        4 of 128 over 500 27    31    20
 // The costs are those of a whole MI355X whatever CUs the stream has, so that the
 // workspace and the results do not depend on it; both ways slow down alike.
 constexpr int kCus = 256;
-constexpr int kFewBlocks = 8;  // (unpacked pages read by more blocks have paid for themselves)
+constexpr size_t kRowBytes = kHeadDim * 4 + 8;
+constexpr int kFewBlocks = 8;  // (pages read by more blocks are unpacked with profit)
 struct FewCost {
-    double fixed, tile, byte;  // us of a call, of a tile of the longest piece, of a byte of partials
+    double fixed, tile, byte;  // us of a call, of a tile of the longest piece, of a byte of partials out or in
 };
-constexpr FewCost kFewCost[2] = {{7.0, 1.6, 0.24e-6}, {10.5, 2.25, 0.21e-6}};
-constexpr FewCost kUnpackCost = {16.5, 0.85, 0.233e-6};  // of a call, of a tile per CU, of a byte of pages
+constexpr FewCost kFewCost[2] = {{6.5, 1.5, 0.33e-6}, {5.6, 2.29, 0.27e-6}};
+// us of a call, of a tile of each CU (a sixteenth of the keys at least: its pieces),
+// of the first tiles, of a byte of pages read, written and read
+constexpr struct {
+    double fixed, tile, first, byte;
+} kUnpackCost = {9.7, 1.03, 0.68, 0.203e-6};
 struct FewPlan {
-    bool use;        // straight from the codes
-    int64_t blocks;  // most query blocks of a (sequence, kv head)
-    int piece_tiles, max_pieces;
-    size_t bytes;    // of workspace
+    int32_t groups;  // work-groups; 0: not straight from the codes
+    int32_t block_rows, piece_tiles, max_pieces;
+    size_t rows, bytes;  // of workspace
 };
 FewPlan few_plan(int32_t batch, const int32_t *h_new_lens, const int32_t *h_prefix_lens, int64_t hkv, int64_t group) {
     FewPlan p{};
-    int64_t rows = 0, tiles = 0, work = 0, most = 0;
-    const auto blocks_of = [&](int32_t b) { return (h_new_lens[b] * group + kBlockRows - 1) / kBlockRows; };
-    const auto tiles_of = [&](int32_t b) {
-        return h_new_lens[b] == 0 ? 0 : (static_cast<int64_t>(h_prefix_lens[b]) + h_new_lens[b] + kTileKeys - 1) / kTileKeys;
+    int64_t tiles = 0, work = 0, max_n = 0;
+    int32_t most = 0;
+    const auto blocks_of = [&](int32_t b) -> int64_t { return (h_new_lens[b] * group + kBlockRows - 1) / kBlockRows; };
+    const auto tiles_of = [&](int32_t b) -> int32_t {
+        return h_new_lens[b] == 0 ? 0 : (h_prefix_lens[b] + h_new_lens[b] + kTileKeys - 1) / kTileKeys;
     };
     for (int32_t b = 0; b < batch; ++b) {
-        rows += h_new_lens[b];
+        if (static_cast<int64_t>(h_prefix_lens[b]) + h_new_lens[b] > int64_t{kTableTiles} * kMaxPieces * kTileKeys) return p;
         tiles += tiles_of(b);
         work += blocks_of(b) * tiles_of(b);
-        p.blocks = std::max(p.blocks, blocks_of(b));
+        max_n = std::max<int64_t>(max_n, h_new_lens[b]);
         most = std::max(most, tiles_of(b));
     }
-    if (rows == 0 || p.blocks > kFewBlocks || most > static_cast<int64_t>(kTableTiles) * kMaxPieces) return p;
+    if (max_n == 0 || max_n * group > kFewBlocks * kBlockRows) return p;
     const double tile_bytes = kTileKeys * kHeadDim * 4 + kTileKeys / kPageSize * (2 * kCodeBytes + kScaleBytes);
-    double best = kUnpackCost.fixed + kUnpackCost.tile * static_cast<double>(work * hkv) / kCus +
+    double best = kUnpackCost.fixed + kUnpackCost.tile * std::max(static_cast<double>(work * hkv) / kCus, static_cast<double>(most) / 16) +
+                  kUnpackCost.first * static_cast<double>(std::min(most, 8)) +
                   kUnpackCost.byte * tile_bytes * static_cast<double>(tiles * hkv);
+    const auto groups = [&](int32_t len) {
+        int64_t sum = 0;
+        for (int32_t b = 0; b < batch; ++b) sum += blocks_of(b) * ((tiles_of(b) + len - 1) / len);
+        return sum * hkv;
+    };
     for (int per_cu = 1; per_cu <= 2; ++per_cu) {
         const int64_t slots = per_cu * kCus;
-        const auto groups = [&](int64_t len) {
-            int64_t sum = 0;
-            for (int32_t b = 0; b < batch; ++b) sum += blocks_of(b) * ((tiles_of(b) + len - 1) / len);
-            return sum * hkv;
-        };
-        // the shortest pieces that all run at once, as far as there are such
-        int64_t lo = std::max<int64_t>(2, (most + kMaxPieces - 1) / kMaxPieces);
-        for (int64_t hi = std::max(lo, std::min<int64_t>(most, kTableTiles)); lo < hi;) {
-            const int64_t mid = (lo + hi) / 2;
-            if (groups(mid) <= slots)
-                hi = mid;
-            else
-                lo = mid + 1;
+        // the shortest pieces that all run at once, or, where many short sequences leave
+        // few places for a long one's, in up to four rounds (4 tokens each over 30000 and
+        // 59 times over 100: 35 us, in one round 325)
+        for (int rounds = 1, last = 0; rounds <= 4; rounds *= 2) {
+            int32_t lo = std::max<int32_t>(2, (most + kMaxPieces - 1) / kMaxPieces);
+            for (int32_t hi = std::max(lo, std::min(most, kTableTiles)); lo < hi;) {
+                const int32_t mid = (lo + hi) / 2;
+                if (groups(mid) <= rounds * slots)
+                    hi = mid;
+                else
+                    lo = mid + 1;
+            }
+            if (lo == last) break;
+            last = lo;
+            const int64_t n = groups(lo), len = std::min(lo, most);
+            if (n > INT32_MAX) break;
+            double moved = 0;  // bytes of partials
+            for (int32_t b = 0; b < batch && lo < most; ++b)
+                if (tiles_of(b) > lo) moved += static_cast<double>(h_new_lens[b]) * hkv * group * ((tiles_of(b) + lo - 1) / lo) * kRowBytes;
+            const FewCost &c = kFewCost[per_cu - 1];
+            const double in_turn = n <= slots ? len : std::min<double>(len * ((n + slots - 1) / slots), len + static_cast<double>(work * hkv) / slots);
+            const double us = c.fixed + c.tile * in_turn + c.byte * 2.0 * moved;
+            if (us >= best) continue;
+            best = us;
+            p.groups = static_cast<int32_t>(n);
+            p.block_rows = static_cast<int32_t>(std::min<int64_t>(kBlockRows, max_n * group));
+            p.piece_tiles = lo;
+            p.max_pieces = (most + lo - 1) / lo;
+            p.rows = lo < most ? static_cast<size_t>(n) * p.block_rows : 0;
+            p.bytes = p.rows * kRowBytes;
         }
-        const int64_t pieces = (most + lo - 1) / lo, rounds = (groups(lo) + slots - 1) / slots;
-        const size_t bytes = pieces > 1 ? static_cast<size_t>(pieces) * rows * hkv * group * (kHeadDim * 4 + 8) : 0;
-        const FewCost &c = kFewCost[per_cu - 1];
-        const double us = c.fixed + c.tile * static_cast<double>(std::min(lo, most) * rounds) + c.byte * 2.0 * static_cast<double>(bytes);
-        if (us >= best) continue;
-        best = us;
-        p.use = true;
-        p.piece_tiles = static_cast<int>(lo);
-        p.max_pieces = static_cast<int>(pieces);
-        p.bytes = bytes;
     }
     return p;
 }
@@ -490,7 +547,7 @@ mw_status mw_kv4_prefill_workspace_size(const mw_attn_shape *shape, int32_t batc
     if (st != MW_OK) return st;
     if (!bytes) return fail(MW_ERR_INVALID_ARG, "%s: bytes is NULL", who);
     const FewPlan few = few_plan(batch, h_new_lens, h_prefix_lens, shape->num_kv_heads, shape->num_q_heads / shape->num_kv_heads);
-    if (few.use) {
+    if (few.groups > 0) {
         *bytes = few.bytes;
         return MW_OK;
     }
@@ -530,25 +587,24 @@ mw_status mw_kv4_prefill_attn(const mw_kv_pool *pool, const mw_attn_shape *shape
         timing_end(timing);
         return st;
     }
-    if (few.use) {
+    if (few.groups > 0) {
         if (workspace_bytes < few.bytes || (few.bytes > 0 && (!d_workspace || !aligned16(d_workspace))))
             return fail(MW_ERR_INVALID_ARG, "%s: needs a 16-byte aligned workspace of %zu bytes (got %zu)", who, few.bytes,
                         workspace_bytes);
         float *ws = static_cast<float *>(d_workspace);
-        const size_t values = static_cast<size_t>(few.max_pieces) * total * shape->num_q_heads;
-        const FewRows rows{ws, reinterpret_cast<float2 *>(ws + values * kHeadDim), total, few.piece_tiles, few.max_pieces};
+        const FewRows rows{ws, reinterpret_cast<float2 *>(ws + few.rows * kHeadDim), few.groups, few.block_rows, few.piece_tiles,
+                           few.max_pieces};
         st = timing_begin(timing, s);
         if (st != MW_OK) return st;
-        hipLaunchKernelGGL(k_kv4_prefill, dim3(static_cast<unsigned>(few.blocks * pl.hkv * few.max_pieces), batch), dim3(256), 0,
-                           s, pool->k4, pool->v4, pool->scales, static_cast<const uint16_t *>(d_q),
-                           static_cast<uint16_t *>(d_out), d_qo_indptr, d_prefix_lens, d_block_table, bt_stride,
-                           Divisor(pl.hkv), Divisor(pl.group), Divisor(static_cast<int>(few.blocks)), pool->desc.num_pages,
-                           pl.scale_log2, rows);
+        hipLaunchKernelGGL(k_kv4_prefill, dim3(static_cast<unsigned>(few.groups)), dim3(256), 0, s, pool->k4, pool->v4,
+                           pool->scales, static_cast<const uint16_t *>(d_q), static_cast<uint16_t *>(d_out), d_qo_indptr,
+                           d_prefix_lens, d_block_table, bt_stride, batch, Divisor(pl.hkv), Divisor(pl.group),
+                           pool->desc.num_pages, pl.scale_log2, rows);
         st = check_launch("k_kv4_prefill");
         if (st == MW_OK) st = timing_kernel_done(timing, s);
         if (st == MW_OK && few.max_pieces > 1) {
             hipLaunchKernelGGL(k_kv4_merge, dim3(static_cast<unsigned>((max_n * shape->num_q_heads + 3) / 4), batch), dim3(256), 0,
-                               s, static_cast<uint16_t *>(d_out), d_qo_indptr, d_prefix_lens, Divisor(shape->num_q_heads),
+                               s, static_cast<uint16_t *>(d_out), d_qo_indptr, d_prefix_lens, Divisor(pl.hkv),
                                Divisor(pl.group), rows);
             st = check_launch("k_kv4_merge");
             if (st == MW_OK) st = timing_kernel_done(timing, s);

@@ -157,8 +157,8 @@ mw_status mw_kv_pool_gather(const mw_kv_pool *pool, const int32_t *d_block_table
 mw_status mw_kv4_pool_create(const mw_kv_pool_desc *desc, void *d_k_codes, void *d_v_codes, void *d_scales,
                              mw_kv_pool **out);
 /* Appends rows, as mw_kv_pool_write does (arguments and checks alike).  Bytes of
- * V codes hold two tokens each: calls that run at the same time may not write
- * tokens of one page. */
+ * V codes hold two tokens each: sequences of a call, and calls that run at the same
+ * time, may not write tokens of one page. */
 mw_status mw_kv4_pool_write(const mw_kv_pool *pool, int32_t batch, const int32_t *h_new_lens,
                             const int32_t *h_start_pos, const int32_t *d_qo_indptr, const int32_t *d_start_pos,
                             const int32_t *d_block_table, int32_t bt_stride, const void *d_k_new, const void *d_v_new,
@@ -179,7 +179,8 @@ mw_status mw_kv4_pool_gather(const mw_kv_pool *pool, int32_t batch, const int32_
  *     (a, c) -> (a cos(t f_i) - c sin(t f_i), c cos(t f_i) + a sin(t f_i))
  * over the pairs i < rot_dim / 2 of y: (y[i], y[i + rot_dim/2]), or
  * (y[2i], y[2i+1]) with `neighbours`; dims from rot_dim on are left.  Computed
- * in fp32 (the angle's product in fp64), rounded to bf16 once.  Queries go to
+ * in fp32 (the angle's product in fp64; the squares of a row have to add up to less
+ * than 2^128), rounded to bf16 once.  Queries go to
  * d_q_out, keys and the values (unchanged) to the pool, which may be of either
  * kind: in 4 bits the rounded key is what is quantised. */
 typedef struct {

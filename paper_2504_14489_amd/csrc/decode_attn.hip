@@ -70,17 +70,20 @@ constexpr int64_t kBalancedMaxUnits = 256;
 struct SplitCost {
     int64_t min_pages;    // the fewest pages a unit streams: a step per wave (short calls are bound by
                           // latency, not bytes, and fewer, longer pieces leave less to merge at the end)
+    int64_t few_pages;    // and where that leaves a segment at most kFewPieces pieces
     int64_t step_pages;   // of a wave
     int64_t merge_steps;  // a merge's time in steps of a wave
     double cu_us, all_us; // a page at a CU's own limit, and at the memory's
 };
-constexpr SplitCost kSplitBf16{16, 2, 3, 0.14, 0.00104};
+constexpr SplitCost kSplitBf16{16, 16, 2, 3, 0.14, 0.00104};
 // In 4 bits: 38 batches of 1 to 256 sequences of 256 to 32768 tokens timed with
-// every split.  Units of 32 pages instead of 16 take one sequence of 8192 tokens
-// of 8 kv heads from 13.3 to 12.0 us, one of 32768 of one kv head from 18.7 to
-// 14.5; whole segments of 3 steps next to ranges of 2 take 24 of 1000 tokens from
-// 16.1 to 13.4, next to ranges of 1 one of 1500 from 11.0 to 11.5.
-constexpr SplitCost kSplitFourBit{32, 4, 1, 0.061, 0.00033};
+// every split.  Units of 16 pages (a step of a wave on each SIMD) instead of 32 take
+// one sequence of 4003 tokens of 8 kv heads from 11.4 to 10.2 us, one of 8192 of one
+// kv head from 11.4 to 10.7, but one of 32768, 128 pieces, from 14.5 to 16.8; whole
+// segments of 3 steps next to ranges of 2 take 24 of 1000 tokens from 16.1 to 13.4,
+// next to ranges of 1 one of 1500 from 11.0 to 11.5.
+constexpr SplitCost kSplitFourBit{32, 16, 4, 1, 0.061, 0.00033};
+constexpr int64_t kFewPieces = 32;
 
 struct Plan {
     int64_t units;            // work-groups of the split kernel
@@ -155,9 +158,13 @@ mw_status plan_decode(const mw_attn_shape *shape, int32_t batch, const int32_t *
         pl->chunk_pages = 0;
         pl->aligned = false;
         const int64_t pages = count(1) * hkv, segs = static_cast<int64_t>(batch) * hkv;
+        int64_t np_max = 0;
+        for (int32_t b = 0; b < batch; ++b)
+            np_max = std::max<int64_t>(np_max, (h_seq_lens[b] + kPageSize - 1) / kPageSize);
+        const int64_t min_pages = np_max <= kFewPieces * cost.few_pages ? cost.few_pages : cost.min_pages;
         // the workspace holds two units per CU's pieces
         const auto ranges = [&](int64_t most) {
-            const int64_t n = std::max<int64_t>(1, std::min(most, (pages + cost.min_pages - 1) / cost.min_pages));
+            const int64_t n = std::max<int64_t>(1, std::min(most, (pages + min_pages - 1) / min_pages));
             return std::max<int64_t>(1, (pages + n - 1) / n);
         };
         const int64_t sized_range = ranges(std::min(2 * std::max<int64_t>(n_cus, 1), kBalancedSizedUnits));
@@ -165,9 +172,6 @@ mw_status plan_decode(const mw_attn_shape *shape, int32_t batch, const int32_t *
         const int64_t most = std::min(kBalancedPerCu * std::max<int64_t>(n_cus, 1), kBalancedMaxUnits);
         pl->per_unit = ranges(most);
         pl->total = pages;
-        int64_t np_max = 0;
-        for (int32_t b = 0; b < batch; ++b)
-            np_max = std::max<int64_t>(np_max, (h_seq_lens[b] + kPageSize - 1) / kPageSize);
         auto padded_units = [&](int64_t r) {
             int64_t n = 0;
             for (int32_t b = 0; b < batch; ++b) n += ((h_seq_lens[b] + kPageSize - 1) / kPageSize + r - 1) / r;
@@ -185,7 +189,7 @@ mw_status plan_decode(const mw_attn_shape *shape, int32_t batch, const int32_t *
                 // Every segment whole in a unit of its own, if its few more
                 // steps (1.3 us each) cost no more than storing, flagging and
                 // merging its pieces (about 4 us).
-                align_to(std::max(cost.min_pages, np_max));
+                align_to(std::max(min_pages, np_max));
             } else {
                 // Pad every segment to a multiple of the range, so that a unit
                 // holds one piece of one segment (a range that straddles two

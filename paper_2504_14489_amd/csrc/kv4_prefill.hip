@@ -133,7 +133,9 @@ mw_status unpack_layout(int32_t batch, const int32_t *h_new_lens, const int32_t 
 //     a lane of the page has four consecutive keys of eight dims, and the product's
 //     k slots of half h are keys 4h .. 4h+3 and 8+4h .. +3 of the 16, as the score
 //     registers hold them, so each dim is one 8-byte store and each operand one
-//     conflict-free 16-byte read.
+//     16-byte read.  Lanes 16 apart store quads of one half and lanes 8 apart flip
+//     their two dims, so that neither store nor read has a bank conflict (with
+//     half of the LDS cycles lost to them, long chunks took 2-4% longer).
 //   * the causal mask by position; online softmax as in the other kernels.
 // K of the next tile and the V codes of the one after it are on their way while a
 // tile is worked on; one barrier a tile.  A piece leaves (m, l) and its unnormalised
@@ -248,7 +250,7 @@ k_kv4_prefill(const uint8_t *__restrict__ kpool, const uint8_t *__restrict__ vpo
 
     // the lane's codes of a tile: K of keys l32 and 32 + l32, blocks half and 2 + half;
     // V of page `wave`, key quad g, dims 32 b + 2 c, + 1
-    const int g = lane >> 4, c = lane & 15;
+    const int g = (lane >> 5) | (lane >> 3 & 2), c = lane & 15;  // (quads of one half of the slots side by side)
     uint4 kc[4], vc = make_uint4(0, 0, 0, 0);
     uint32_t ks[4], vs[kBlocks] = {0, 0, 0, 0};
     const uint8_t *const k_lane = kpool + (l32 & 15) * 64 + half * 16;
@@ -268,7 +270,7 @@ k_kv4_prefill(const uint8_t *__restrict__ kpool, const uint8_t *__restrict__ vpo
     };
     const auto load_v = [&](int t) __attribute__((always_inline)) {
         const size_t block = max(__builtin_amdgcn_readfirstlane(s_bt[4 * (t - t_lo) + wave]), 0);
-        vc = *reinterpret_cast<const uint4 *>(vpool + block * kCodeBytes + lane * 16);
+        vc = *reinterpret_cast<const uint4 *>(vpool + block * kCodeBytes + g * 256 + c * 16);
         const uint8_t *sc = scales + block * kScaleBytes + kBlocks * kPageSize + 4 * g;
 #pragma unroll
         for (int i = 0; i < kBlocks; ++i) vs[i] = *reinterpret_cast<const uint32_t *>(sc + i * kPageSize);
@@ -284,12 +286,13 @@ k_kv4_prefill(const uint8_t *__restrict__ kpool, const uint8_t *__restrict__ vpo
         for (int i = 0; i < kBlocks; ++i) bytes[i] = vs[i] & mask;
         decode_v(codes, bytes, v);
         char *dst = buf + (2 * wave + (g & 1)) * 512 + c * 32 + (g >> 1) * 8;
+        const int flip = 16 * (c >> 3);
 #pragma unroll
         for (int i = 0; i < kBlocks; ++i) {
             // two dims of four keys each to four keys of two dims
-            *reinterpret_cast<uint2 *>(dst + i * 4096) =
+            *reinterpret_cast<uint2 *>(dst + i * 4096 + flip) =
                 make_uint2(__builtin_amdgcn_perm(v[1][i], v[0][i], 0x05040100), __builtin_amdgcn_perm(v[3][i], v[2][i], 0x05040100));
-            *reinterpret_cast<uint2 *>(dst + i * 4096 + 16) =
+            *reinterpret_cast<uint2 *>(dst + i * 4096 + 16 - flip) =
                 make_uint2(__builtin_amdgcn_perm(v[1][i], v[0][i], 0x07060302), __builtin_amdgcn_perm(v[3][i], v[2][i], 0x07060302));
         }
     };
@@ -374,7 +377,7 @@ k_kv4_prefill(const uint8_t *__restrict__ kpool, const uint8_t *__restrict__ vpo
                 l_run += ((w[0] + w[1]) + (w[2] + w[3])) + ((w[4] + w[5]) + (w[6] + w[7]));
                 p[s] = __builtin_bit_cast(bf16x8, make_uint4(cvt2(w[0], w[1]), cvt2(w[2], w[3]), cvt2(w[4], w[5]), cvt2(w[6], w[7])));
             }
-            const char *vb = s_v[(t - t_lo) & 1] + half * 512 + l32 * 16;
+            const char *vb = s_v[(t - t_lo) & 1] + half * 512 + (l32 ^ l32 >> 4) * 16;
 #pragma unroll
             for (int s = 0; s < 4; ++s)
 #pragma unroll

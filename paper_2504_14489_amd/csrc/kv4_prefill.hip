@@ -118,7 +118,7 @@ mw_status unpack_layout(int32_t batch, const int32_t *h_new_lens, const int32_t 
 // ------------------------------------------------------- few rows: straight from the codes
 // A chunk of few rows reads each page for few query blocks, so unpacking it to
 // bf16 first (write 8192 bytes, read them again) costs more than it saves: 64
-// tokens over 8000 of 32/8 heads take 26 us like this and 37 unpacked, 16 tokens 18
+// tokens over 8000 of 32/8 heads take 25 us like this and 37 unpacked, 16 tokens 18
 // and 34.  A tile takes 1.5 us of a CU with one work-group, 1.1 of each of two; it
 // is bound by the instructions that its four waves issue, not by memory (reading
 // the same tile over and over changes nothing; without the conversions it is 15-20%

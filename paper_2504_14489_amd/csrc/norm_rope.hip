@@ -142,8 +142,8 @@ __device__ __forceinline__ int each_row(uint4 x, int group, int step, int t0, in
 // and lie in LDS; then 16 lanes take a head row at a time.  Quads, because V in 4
 // bits is stored by four tokens (kv4_format.h).
 // Measured (kernel alone): 4096 tokens of 32 + 2 * 8 heads into bf16, 101 MB, 23 us
-// (a copy of as many bytes 21); 9275 of 64 + 2 * 8 into 4 bits, 362 MB, 93 us.
-// Six work-groups per CU: with the registers of five the latter takes 99.
+// (a copy of as many bytes 21); 10315 of 64 + 2 * 8 into 4 bits, 391 MB, 90 us (a copy
+// 80).  Six work-groups per CU: with the registers of five the latter takes 6% longer.
 template <bool kFourBit, Pairing kPairing>
 __global__ void __launch_bounds__(256, 6)
 k_norm_rope(NormRopeArgs a, Cache kv, const int32_t *__restrict__ indptr, const int32_t *__restrict__ start_pos) {

@@ -580,3 +580,94 @@ def test_prefill_in_a_graph_with_eager_calls_between():
     finally:
         for p in calls:
             p.close()
+
+
+def test_two_calls_at_a_time():
+    """A decode batch and a chunk on two streams, with workspaces of their own: what each gives alone."""
+    say("kv4 two streams")
+    d, p = Decode(32, 8, [3000, 50, 1700, 900], seed=61), Prefill(32, 8, [40, 7], [3000, 100], seed=62)
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    try:
+        d.run()
+        p.run()
+        torch.cuda.synchronize()
+        alone = [R.bits_of(d.out), R.bits_of(p.out)]
+        for _ in range(8):
+            d.out.fill_(0x1234)
+            p.out.fill_(0x1234)
+            torch.cuda.synchronize()
+            for _ in range(4):
+                d.run(streams[0].cuda_stream)
+                p.run(streams[1].cuda_stream)
+            torch.cuda.synchronize()
+            assert np.array_equal(R.bits_of(d.out)[:4], alone[0][:4])
+            assert np.array_equal(R.bits_of(p.out)[:47], alone[1][:47])
+        d.check("decode beside a chunk")
+        p.check()
+    finally:
+        d.pool.close()
+        p.close()
+
+
+def test_a_pool_past_32_bits():
+    """Rows on the last pages of a pool whose codes take more than 4 GiB: every call as on a small pool."""
+    say("kv4 large pool")
+    hq, hkv, lens = 8, 4, [1030, 5]
+    rng = np.random.Generator(np.random.PCG64(71))
+    table, pages = R.tables(lens, rng)
+    far = (1 << 32) // (hkv * 1024) + 100
+    k, v = (R.device(normal_bits(rng, sum(lens), hkv, 128).view(np.int16)) for _ in range(2))
+    x = R.device(normal_bits(rng, 2, hq + 2 * hkv, 128).view(np.int16))
+    q = R.device(normal_bits(rng, 602, hq, 128).view(np.int16))
+    freq = R.device(1e4 ** (-np.arange(64, dtype=np.float64) / 64))
+    got = []
+    for shift in (0, far):
+        total = pages + shift
+        k4, v4 = (torch.empty(total, hkv, 1024, dtype=torch.uint8, device="cuda") for _ in range(2))
+        scales = torch.empty(total, hkv, 128, dtype=torch.uint8, device="cuda")
+        assert shift == 0 or k4.numel() > 1 << 32
+        for t in (k4, v4, scales):
+            t[-pages:].zero_()
+        pool = mw.mw_kv4_pool_create(total, 16, hkv, 128, k4.data_ptr(), v4.data_ptr(), scales.data_ptr())
+        try:
+            bt = table + shift
+            dbt, zero, ip = R.device(bt), R.device([0, 0], np.int32), rows(lens)
+            place = (np.array(lens, np.int32), np.zeros(2, np.int32), ip.data_ptr(), zero.data_ptr(), dbt.data_ptr(),
+                     bt.shape[1])
+            mw.mw_kv4_pool_write(pool, *place, k.data_ptr(), v.data_ptr())
+            # one token of each again, through the norm and rotation
+            last, ones, ip1 = np.array(lens, np.int32) - 1, np.ones(2, np.int32), rows([1, 1])
+            dlast, q_out = R.device(last), torch.empty(2, hq, 128, dtype=torch.int16, device="cuda")
+            rope = mw.NormRope(num_q_heads=hq, rot_dim=128, neighbours=0, eps=1e-6, d_q_weight=0, d_k_weight=0,
+                               d_inv_freq=freq.data_ptr())
+            at, stride = x.data_ptr(), (hq + 2 * hkv) * 128
+            mw.mw_qk_norm_rope_write(pool, rope, ones, last, ip1.data_ptr(), dlast.data_ptr(), dbt.data_ptr(),
+                                     bt.shape[1], at, stride, at + 256 * hq, stride, at + 256 * (hq + hkv), stride,
+                                     q_out.data_ptr())
+            ko, vo = torch.empty_like(k), torch.empty_like(v)
+            mw.mw_kv4_pool_gather(pool, *place, ko.data_ptr(), vo.data_ptr())
+            out = [q_out, ko, vo]
+            dlens, o = R.device(lens, np.int32), torch.empty(2, hq, 128, dtype=torch.int16, device="cuda")
+            n = mw.mw_kv4_decode_workspace_size(hq, hkv, 128, lens)
+            ws = torch.empty(n, dtype=torch.uint8, device="cuda")
+            mw.mw_kv4_decode_attn(pool, hq, hkv, 128, SCALE, lens, dlens.data_ptr(), dbt.data_ptr(), bt.shape[1],
+                                  q.data_ptr(), o.data_ptr(), ws.data_ptr(), n)
+            out.append(o)
+            for new in ([20, 2], [600, 2]):  # straight from the codes, and unpacked
+                prefix = [m - c for m, c in zip(lens, new)]
+                ipn, dpre = rows(new), R.device(prefix, np.int32)
+                n = mw.mw_kv4_prefill_workspace_size(hq, hkv, 128, new, prefix)
+                ws2 = torch.empty(max(n, 16), dtype=torch.uint8, device="cuda")
+                o = torch.empty(sum(new), hq, 128, dtype=torch.int16, device="cuda")
+                mw.mw_kv4_prefill_attn(pool, hq, hkv, 128, SCALE, new, prefix, ipn.data_ptr(), dpre.data_ptr(),
+                                       dbt.data_ptr(), bt.shape[1], q.data_ptr(), o.data_ptr(), ws2.data_ptr(), n)
+                torch.cuda.synchronize()
+                out.append(o)
+            torch.cuda.synchronize()
+            got.append([R.bits_of(t) for t in out])
+        finally:
+            torch.cuda.synchronize()
+            mw.mw_kv_pool_destroy(pool)
+        del k4, v4, scales
+    for a, b in zip(*got):
+        assert np.isfinite(bits_to_f32(a)).all() and a.any() and np.array_equal(a, b)

@@ -329,3 +329,58 @@ def test_a_layer_from_projection_to_output(four_bit):
     finally:
         torch.cuda.synchronize()
         mw.mw_kv_pool_destroy(handle)
+
+
+@pytest.mark.parametrize("four_bit", [False, True])
+def test_a_decode_step_in_a_graph_with_eager_steps_between(four_bit):
+    """Norm, rotation, append and decode attention of one token of each sequence, captured; replayed on other rows,
+    against an eager step on them."""
+    say(f"layer graph four_bit={four_bit}")
+    hq, hkv, starts = 8, 2, [700, 0, 33, 1900]
+    r = Rows(hq, hkv, [1] * 4, starts, four_bit, seed=3)
+    lens = np.array(starts, np.int32) + 1
+    dlens, out = R.device(lens), torch.zeros(4, hq, 128, dtype=torch.int16, device="cuda")
+    # the sequences' earlier pages: any page of the pool, read by both sides
+    table = np.where(r.table < 0, 0, r.table)
+    r.table, r.dtable = table, R.device(table)
+    size = (mw.mw_kv4_decode_workspace_size if four_bit else mw.mw_decode_workspace_size)(hq, hkv, 128, lens)
+    ws = torch.full((size,), 0xFF, dtype=torch.uint8, device="cuda")
+    stream = torch.cuda.Stream()
+
+    def step():
+        at = r.rows.data_ptr()
+        stride = r.rows.shape[1]
+        mw.mw_qk_norm_rope_write(r.handle, r.rope, *r.place(), at, stride, at + 256 * hq, stride,
+                                 at + 256 * (hq + hkv), stride, r.q_out.data_ptr(), stream.cuda_stream)
+        args = (r.handle, hq, hkv, 128, 128**-0.5, lens, dlens.data_ptr(), r.dtable.data_ptr(), table.shape[1],
+                r.q_out.data_ptr(), out.data_ptr(), ws.data_ptr(), size)
+        if four_bit:
+            mw.mw_kv4_decode_attn(*args, stream.cuda_stream)
+        else:
+            mw.mw_decode_attn(*args, 0, stream.cuda_stream)
+
+    try:
+        torch.cuda.synchronize()
+        step()
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=stream):
+            step()
+        gen = torch.Generator(device="cuda").manual_seed(9)
+        for _ in range(4):
+            fresh = torch.randn(r.rows.shape, generator=gen, device="cuda").bfloat16().view(torch.int16)
+            r.rows.copy_(fresh)
+            out.zero_()
+            torch.cuda.synchronize()
+            with torch.cuda.stream(stream):
+                graph.replay()
+            torch.cuda.synchronize()
+            replayed = R.bits_of(out)
+            assert np.isfinite(bits_to_f32(replayed)).all() and replayed.any()
+            out.zero_()
+            torch.cuda.synchronize()
+            step()
+            torch.cuda.synchronize()
+            assert np.array_equal(R.bits_of(out), replayed)
+    finally:
+        r.close()

@@ -72,17 +72,18 @@ struct SplitCost {
                           // latency, not bytes, and fewer, longer pieces leave less to merge at the end)
     int64_t few_pages;    // and where that leaves a segment at most kFewPieces pieces
     int64_t step_pages;   // of a wave
+    int64_t pad_pages;    // segments and units of the balanced split are multiples of so many pages
     int64_t merge_steps;  // a merge's time in steps of a wave
     double cu_us, all_us; // a page at a CU's own limit, and at the memory's
 };
-constexpr SplitCost kSplitBf16{16, 16, 2, 3, 0.14, 0.00104};
+constexpr SplitCost kSplitBf16{16, 16, 2, 1, 3, 0.14, 0.00104};
 // In 4 bits: 38 batches of 1 to 256 sequences of 256 to 32768 tokens timed with
 // every split.  Units of 16 pages (a step of a wave on each SIMD) instead of 32 take
 // one sequence of 4003 tokens of 8 kv heads from 11.4 to 10.2 us, one of 8192 of one
 // kv head from 11.4 to 10.7, but one of 32768, 128 pieces, from 14.5 to 16.8; whole
 // segments of 3 steps next to ranges of 2 take 24 of 1000 tokens from 16.1 to 13.4,
 // next to ranges of 1 one of 1500 from 11.0 to 11.5.
-constexpr SplitCost kSplitFourBit{32, 16, 4, 1, 0.061, 0.00033};
+constexpr SplitCost kSplitFourBit{32, 16, 4, 4, 1, 0.061, 0.00033};
 constexpr int64_t kFewPieces = 32;
 
 struct Plan {
@@ -157,7 +158,8 @@ mw_status plan_decode(const mw_attn_shape *shape, int32_t batch, const int32_t *
     auto balanced = [&](int64_t n_cus, Plan *pl, bool may_align) {
         pl->chunk_pages = 0;
         pl->aligned = false;
-        const int64_t pages = count(1) * hkv, segs = static_cast<int64_t>(batch) * hkv;
+        const int64_t pad = cost.pad_pages, segs = static_cast<int64_t>(batch) * hkv;
+        const int64_t pages = count(static_cast<int>(pad)) * pad * hkv;
         int64_t np_max = 0;
         for (int32_t b = 0; b < batch; ++b)
             np_max = std::max<int64_t>(np_max, (h_seq_lens[b] + kPageSize - 1) / kPageSize);
@@ -165,7 +167,7 @@ mw_status plan_decode(const mw_attn_shape *shape, int32_t batch, const int32_t *
         // the workspace holds two units per CU's pieces
         const auto ranges = [&](int64_t most) {
             const int64_t n = std::max<int64_t>(1, std::min(most, (pages + min_pages - 1) / min_pages));
-            return std::max<int64_t>(1, (pages + n - 1) / n);
+            return std::max(pad, ((pages + n - 1) / n + pad - 1) / pad * pad);
         };
         const int64_t sized_range = ranges(std::min(2 * std::max<int64_t>(n_cus, 1), kBalancedSizedUnits));
         const int64_t sized = (pages + sized_range - 1) / sized_range;
@@ -312,6 +314,16 @@ mw_status mw_decode_workspace_size(const mw_attn_shape *shape, int32_t batch, co
     if (!bytes) return fail(MW_ERR_INVALID_ARG, "mw_decode_workspace_size: bytes is NULL");
     Plan pl;
     mw_status st = plan_decode(shape, batch, h_seq_lens, chunk_pages, 0, -1, &pl, "mw_decode_workspace_size");
+    if (st != MW_OK) return st;
+    *bytes = pl.bytes;
+    return MW_OK;
+}
+
+mw_status mw_kv4_decode_workspace_size(const mw_attn_shape *shape, int32_t batch, const int32_t *h_seq_lens, size_t *bytes) {
+    const char *who = "mw_kv4_decode_workspace_size";
+    if (!bytes) return fail(MW_ERR_INVALID_ARG, "%s: bytes is NULL", who);
+    Plan pl;
+    const mw_status st = plan_decode(shape, batch, h_seq_lens, 0, 0, -1, &pl, who, kSplitFourBit);
     if (st != MW_OK) return st;
     *bytes = pl.bytes;
     return MW_OK;

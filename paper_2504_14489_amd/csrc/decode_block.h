@@ -651,11 +651,12 @@ finish_segments(uint16_t *__restrict__ out, const float *__restrict__ ws_o, cons
 }
 
 // A wave's share of a unit's pages, given out in chunks of up to 64 consecutive
-// pages of one segment.  kRound: shares of up to four steps of as many pages are
-// whole steps, so that a short unit keeps fewer waves busy instead of all of them
-// with steps in part empty (in 4 bits, where a step's instructions take 1 us of a
-// SIMD's time: a unit of 16 pages 1.5 us instead of 2.8).
-template <int kRound = 1>
+// pages of one segment.  kStep > 1: in whole steps of as many pages, in a numbering
+// that pads each segment to them (a wave's step costs the same however few of its
+// pages there are; in 4 bits 1 us of a SIMD's time): a wave's steps are then those
+// of its share, wherever segments end in it, and a short unit keeps fewer waves
+// busy instead of all of them with steps in part empty.
+template <int kStep = 1>
 struct SpanShare {
     struct Chunk {
         int b, kvh, p, p_end, np, len, first;
@@ -665,12 +666,13 @@ struct SpanShare {
     int bt_stride, hkv, batch, lane;
     Lengths len;
     int b, np, kvh, off, seg_len, seg_first, left;  // left: pages of the share not yet given to a chunk
+    __device__ __forceinline__ static int padded(int pages) { return (pages + kStep - 1) / kStep * kStep; }
 
     __device__ __forceinline__ SpanShare(const int32_t *seq_lens, const int32_t *bt_, int bt_stride_, int batch_, int hkv_,
                                          int per_unit, int total, bool aligned, int u, int wave, int lane_)
         : bt(bt_), bt_stride(bt_stride_), hkv(hkv_), batch(batch_), lane(lane_), len{seq_lens, batch_, bt_stride_, 0, 0},
           b(0), np(0), kvh(0), off(0), seg_len(0), seg_first(0), left(0) {
-        const int align = aligned ? per_unit : 0;
+        const int align = aligned ? per_unit : kStep > 1 ? kStep : 0;
         // this wave's share [g, g_end) and where it starts
         const int u0 = u * per_unit;
         int u1 = min(u0 + per_unit, total);
@@ -679,7 +681,7 @@ struct SpanShare {
             if (!locate_page(len, hkv, align, g, b, base)) return false;
             seg_len = len.at(b);
             np = Lengths::pages(seg_len);
-            nv = aligned ? (np + align - 1) / align * align : np;
+            nv = aligned ? (np + align - 1) / align * align : padded(np);
             kvh = (g - base) / nv;
             seg_first = base + kvh * nv;
             off = g - seg_first;
@@ -690,12 +692,16 @@ struct SpanShare {
             live = at_page(u0);
             u1 = u0 + min(per_unit, np - off);  // the padding holds no pages
         }
-        int share = (u1 - u0 + kSpanWaves - 1) / kSpanWaves;
-        if (kRound > 1 && share <= 4 * kRound) share = (share + kRound - 1) / kRound * kRound;
-        const int g = u0 + wave * share;
+        int share = (u1 - u0 + kSpanWaves - 1) / kSpanWaves, before = wave * share;
+        if constexpr (kStep > 1) {  // the first waves take a step more
+            const int steps = (u1 - u0 + kStep - 1) / kStep, more = steps % kSpanWaves;
+            share = (steps / kSpanWaves + (wave < more ? 1 : 0)) * kStep;
+            before = (wave * (steps / kSpanWaves) + min(wave, more)) * kStep;
+        }
+        const int g = u0 + before;
         left = live ? min(share, u1 - g) : 0;
         if (aligned)
-            off += wave * share;
+            off += before;
         else if (left > 0 && !at_page(g))
             left = 0;
     }
@@ -706,9 +712,10 @@ struct SpanShare {
         c.p_end = off + n;
         left -= n;
         off += n;
+        if (kStep > 1 && off == np) left -= padded(np) - np;
         if (off == np && left > 0) {  // on to the next segment
             off = 0;
-            seg_first += np;
+            seg_first += padded(np);
             if (++kvh == hkv) {
                 kvh = 0;
                 if (++b < batch) {

@@ -430,11 +430,6 @@ k_kv4_decode(const uint8_t *__restrict__ kpool, const uint8_t *__restrict__ vpoo
 
 extern "C" {
 
-mw_status mw_kv4_decode_workspace_size(const mw_attn_shape *shape, int32_t batch, const int32_t *h_seq_lens,
-                                       size_t *bytes) {
-    return mw_decode_workspace_size(shape, batch, h_seq_lens, 0, bytes);
-}
-
 mw_status mw_kv4_decode_attn(const mw_kv_pool *pool, const mw_attn_shape *shape, int32_t batch,
                              const int32_t *h_seq_lens, const int32_t *d_seq_lens, const int32_t *d_block_table,
                              int32_t bt_stride, const void *d_q, void *d_out, void *d_workspace, size_t workspace_bytes,

@@ -60,12 +60,25 @@ __device__ __forceinline__ float split_q(const uint4 (&x)[4 * N], i32x8 (&hi)[N]
 // Weighted sum of the fragments or pieces of one head in a wave: (m, l) of up to
 // 64 of them one per lane, which gives every weight 2^(m - M) and the denominator
 // within the wave, then two outputs per lane.  Those without keys have l = 0 and
-// contribute nothing.  load_o(j): the lane's two values of the j-th, j < n.
+// contribute nothing.  load_o(j): the lane's two values of the j-th, j < n.  The
+// first 8 kBatches of them are requested before (m, l) is looked at: one latency
+// instead of two or three.
 struct HeadSum {
     float M = -INFINITY, L = 0.f;
     float2 acc = make_float2(0.f, 0.f);
-    template <class LoadO>
+    template <int kBatches = 1, class LoadO>
     __device__ __forceinline__ void add(float2 ml, int n, int lane, const LoadO &load_o) {
+        float2 o[8 * kBatches];
+        const auto load = [&](int j0) __attribute__((always_inline)) {
+#pragma unroll
+            for (int i = 0; i < kBatches; ++i)
+                if (i == 0 || j0 + 8 * i < n)
+#pragma unroll
+                    for (int k = 8 * i; k < 8 * i + 8; ++k) o[k] = load_o(min(j0 + k, n - 1));
+        };
+#pragma unroll
+        for (int k = 8; k < 8 * kBatches; ++k) o[k] = make_float2(0.f, 0.f);
+        load(0);
         const bool in = lane < n && ml.y != 0.f;
         const float top = fmaxf(M, wave_max(in ? ml.x : -INFINITY));
         const float old = L == 0.f ? 0.f : __builtin_amdgcn_exp2f(M - top);
@@ -74,18 +87,18 @@ struct HeadSum {
         L = L * old + wave_sum(in ? w * ml.y : 0.f);
         acc.x *= old;
         acc.y *= old;
-#pragma unroll 1
-        for (int j0 = 0; j0 < n; j0 += 8) {
-            float2 o[8];
+        for (int j0 = 0;;) {
 #pragma unroll
-            for (int k = 0; k < 8; ++k) o[k] = load_o(min(j0 + k, n - 1));
-#pragma unroll
-            for (int k = 0; k < 8; ++k) {
+            for (int k = 0; k < 8 * kBatches; ++k) {
+                if (k >= 8 && k % 8 == 0 && j0 + k >= n) break;
                 // lanes from n on have weight 0, and j0 + k < 64
                 const float wk = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, w), j0 + k));
                 acc.x += wk * o[k].x;
                 acc.y += wk * o[k].y;
             }
+            j0 += 8 * kBatches;
+            if (j0 >= n) break;
+            load(j0);
         }
     }
 };

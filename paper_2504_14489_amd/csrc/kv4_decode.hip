@@ -170,7 +170,7 @@ finish_unit(uint16_t *__restrict__ out, float *__restrict__ ws_o, float2 *__rest
             const int n = min(p.nch - jb, 64);
             const float2 ml = __builtin_bit_cast(
                 float2, __hip_atomic_load(ml_src + (jb + min(lane, n - 1)) * group, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
-            s.add(ml, n, lane, [&](int k) __attribute__((always_inline)) {
+            s.add<2>(ml, n, lane, [&](int k) __attribute__((always_inline)) {
                 return __builtin_bit_cast(float2, __hip_atomic_load(o_src + static_cast<int64_t>(jb + k) * step, __ATOMIC_RELAXED,
                                                                     __HIP_MEMORY_SCOPE_AGENT));
             });

@@ -24,12 +24,12 @@ using namespace kv4;
 //     one each; a tile's columns of other blocks are not used.
 // kHeads: 4, 8 or 16, the most query heads of a kv head.
 //
-// Measured: 32 sequences of 16K to 32K tokens of 8 kv heads, 843 MB, 136 us (6.2 TB/s;
-// a plain read reaches 6.5), where memory bounds it.  64 of 512 to 4096, 141 MB, 33.9,
-// and 128 of 64 to 16K of one kv head with 8 query heads, 29 MB, 16.7: a CU's waves
+// Measured: 32 sequences of 16K to 32K tokens of 8 kv heads, 843 MB, 133.5 us (6.3 TB/s;
+// a plain read reaches 6.5), where memory bounds it.  64 of 512 to 4096, 141 MB, 31.7,
+// and 128 of 64 to 16K of one kv head with 8 query heads, 29 MB, 14.6: a CU's waves
 // issue a page in 0.061 us, and 8 to 10 us pass in a start (lengths, table, pages:
 // dependent loads) and an end (pieces, flags, merge) on which nothing else waits.
-// One of 4003 tokens, 4.4 MB, takes 11 and has little else.
+// One of 4003 tokens, 4.4 MB, takes 9.3 and has little else.
 //
 // A unit has eight waves, with steps of four pages: sixteen with steps of two (128
 // registers, the scores' bookkeeping twice as often) took 41 us for 32 sequences

@@ -35,6 +35,7 @@ struct Cache {
     int bt_stride, num_pages, hkv;
 };
 
+typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 __device__ __forceinline__ float lo(uint32_t x) { return __builtin_bit_cast(float, x << 16); }
 __device__ __forceinline__ float hi(uint32_t x) { return __builtin_bit_cast(float, x & 0xffff0000u); }
 __device__ __forceinline__ uint32_t pack2(float a, float b) {
@@ -142,9 +143,10 @@ __device__ __forceinline__ int each_row(uint4 x, int group, int step, int t0, in
 // and lie in LDS; then 16 lanes take a head row at a time.  Quads, because V in 4
 // bits is stored by four tokens (kv4_format.h).
 // Measured (kernel alone): 4096 tokens of 32 + 2 * 8 heads into bf16, 101 MB, 23 us
-// (a copy of as many bytes 21); 10315 of 64 + 2 * 8 into 4 bits, 391 MB, 90 us (a copy
+// (a copy of as many bytes 21); 10315 of 64 + 2 * 8 into 4 bits, 391 MB, 82 us (a copy
 // 80).  Six work-groups per CU: with the registers of five the latter takes 6% longer.
-template <bool kFourBit, Pairing kPairing>
+// kPassBy: rows are read and queries stored past the caches.
+template <bool kFourBit, Pairing kPairing, bool kPassBy>
 __global__ void __launch_bounds__(256, 6)
 k_norm_rope(NormRopeArgs a, Cache kv, const int32_t *__restrict__ indptr, const int32_t *__restrict__ start_pos) {
     __shared__ __attribute__((aligned(16))) Shared sh;
@@ -175,7 +177,10 @@ k_norm_rope(NormRopeArgs a, Cache kv, const int32_t *__restrict__ indptr, const 
         const auto source = [&](const uint16_t *from, int stride) __attribute__((always_inline)) {
             return [=](int h, int t) __attribute__((always_inline)) {
                 const int off = ((t & 1) ? stride : 0) + ((t & 2) ? 2 * stride : 0) + h * kHeadDim + 8 * c;
-                return *reinterpret_cast<const uint4 *>(from + off);
+                if constexpr (kPassBy)
+                    return __builtin_bit_cast(uint4, __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(from + off)));
+                else
+                    return *reinterpret_cast<const uint4 *>(from + off);
             };
         };
         const auto load_q = source(q_src, static_cast<int>(a.q_stride)), load_k = source(k_src, static_cast<int>(a.k_stride));
@@ -193,8 +198,12 @@ k_norm_rope(NormRopeArgs a, Cache kv, const int32_t *__restrict__ indptr, const 
         }
         __syncthreads();
         group = each_row(q_row, group, step, t0, m, a.hq, load_q, [&](int h, int t, uint4 v) __attribute__((always_inline)) {
-            *reinterpret_cast<uint4 *>(q_dst + (static_cast<int>(__umul24(t, a.hq)) + h) * kHeadDim + 8 * c) =
-                norm_rope_row<kPairing>(v, a.q_weight != nullptr, sh.weight[0], a.eps, a.rot_dim, sh, t, c);
+            const uint4 y = norm_rope_row<kPairing>(v, a.q_weight != nullptr, sh.weight[0], a.eps, a.rot_dim, sh, t, c);
+            uint16_t *dst = q_dst + (static_cast<int>(__umul24(t, a.hq)) + h) * kHeadDim + 8 * c;
+            if constexpr (kPassBy)
+                __builtin_nontemporal_store(__builtin_bit_cast(u32x4, y), reinterpret_cast<u32x4 *>(dst));
+            else
+                *reinterpret_cast<uint4 *>(dst) = y;
         });
         if (!held) continue;
         const uint4 k_row = row_of(group, t0, m, kv.hkv, load_k);
@@ -222,6 +231,22 @@ k_norm_rope(NormRopeArgs a, Cache kv, const int32_t *__restrict__ indptr, const 
             });
         }
     }
+}
+
+// Rows and queries of more bytes than these, half of the last cache, go past the
+// caches: queries will not be found there, and would take the place of rows that the
+// projection has just written and this kernel still has to read.  Rows written by a
+// copy just before, 32 + 2 * 8 heads, us past the caches and through them: 512 tokens
+// 10.3 and 10.2, 4096 (84 MB) 20.9 and 20.6, 8192 (168 MB) 40 and 42, 16384 73 and 83;
+// the 10315 of 64 + 2 * 8 heads above, behind nothing, 82 and 90.
+constexpr int64_t kThroughBytes = int64_t{128} << 20;
+
+using Kernel = void (*)(NormRopeArgs, Cache, const int32_t *, const int32_t *);
+template <bool kFourBit, bool kPassBy>
+Kernel kernel_of(const mw_norm_rope &rope) {
+    return rope.neighbours              ? k_norm_rope<kFourBit, kNeighbours, kPassBy>
+           : rope.rot_dim == kHeadDim ? k_norm_rope<kFourBit, kWholeHalves, kPassBy>
+                                      : k_norm_rope<kFourBit, kHalves, kPassBy>;
 }
 
 }  // namespace
@@ -275,9 +300,9 @@ extern "C" mw_status mw_qk_norm_rope_write(const mw_kv_pool *pool, const mw_norm
                              static_cast<int>(hq), static_cast<uint16_t *>(d_q_out)};
         const Cache kv{pool->k, pool->v, pool->k4, pool->v4, pool->scales, d_block_table, bt_stride,
                        pool->desc.num_pages, pool->desc.num_kv_heads};
-        auto kernel = rope->neighbours          ? (pool->k4 ? k_norm_rope<true, kNeighbours> : k_norm_rope<false, kNeighbours>)
-                      : rope->rot_dim == kHeadDim ? (pool->k4 ? k_norm_rope<true, kWholeHalves> : k_norm_rope<false, kWholeHalves>)
-                                                  : (pool->k4 ? k_norm_rope<true, kHalves> : k_norm_rope<false, kHalves>);
+        const bool past = total * (2 * hq + 2 * hkv) * kHeadDim * 2 > kThroughBytes;
+        const Kernel kernel = pool->k4 ? (past ? kernel_of<true, true>(*rope) : kernel_of<true, false>(*rope))
+                                       : (past ? kernel_of<false, true>(*rope) : kernel_of<false, false>(*rope));
         hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(blocks), batch, static_cast<unsigned>(slices)), dim3(256), 0, s, a,
                            kv, d_qo_indptr, d_start_pos);
         st = check_launch("k_norm_rope");

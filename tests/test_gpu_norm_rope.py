@@ -384,3 +384,31 @@ def test_a_decode_step_in_a_graph_with_eager_steps_between(four_bit):
             assert np.array_equal(R.bits_of(out), replayed)
     finally:
         r.close()
+
+
+@pytest.mark.parametrize("four_bit", [False, True])
+@pytest.mark.parametrize("rot,neighbours", [(128, False), (64, False), (128, True)])
+def test_a_call_larger_than_the_caches_as_its_parts(four_bit, rot, neighbours):
+    """Rows and queries of more than 128 MB in one call, and as calls of a few sequences each."""
+    say(f"norm rope large four_bit={four_bit} rot={rot} neighbours={neighbours}")
+    hq, hkv, lens, starts = 64, 4, [1500, 1, 1101, 600, 777], [5, 0, 16, 3, 100]
+    whole, parts = (Rows(hq, hkv, lens, starts, four_bit, rot=rot, neighbours=neighbours, seed=17) for _ in range(2))
+    assert whole.total * (2 * hq + 2 * hkv) * 256 > 128 << 20
+    try:
+        whole.run()
+        row, stride = 0, parts.rows.shape[1]
+        for b in range(len(lens)):
+            one = slice(b, b + 1)
+            at = parts.rows[row:].data_ptr()
+            indptr, start = R.device([0, lens[b]], np.int32), R.device(starts[one], np.int32)
+            mw.mw_qk_norm_rope_write(parts.handle, parts.rope, parts.lens[one], parts.starts[one], indptr.data_ptr(),
+                                     start.data_ptr(), parts.dtable[b].data_ptr(), parts.table.shape[1], at, stride,
+                                     at + 256 * hq, stride, at + 256 * (hq + hkv), stride, parts.q_out[row:].data_ptr())
+            row += lens[b]
+            torch.cuda.synchronize()
+        assert torch.equal(whole.q_out, parts.q_out) and (R.bits_of(whole.q_out[row:]) == 0x1234).all()
+        for a, b in zip(whole.cache_rows(), parts.cache_rows()):
+            assert np.isfinite(a).all() and np.array_equal(a, b)
+    finally:
+        whole.close()
+        parts.close()

@@ -693,10 +693,15 @@ struct SpanShare {
             u1 = u0 + min(per_unit, np - off);  // the padding holds no pages
         }
         int share = (u1 - u0 + kSpanWaves - 1) / kSpanWaves, before = wave * share;
-        if constexpr (kStep > 1) {  // the first waves take a step more
-            const int steps = (u1 - u0 + kStep - 1) / kStep, more = steps % kSpanWaves;
-            share = (steps / kSpanWaves + (wave < more ? 1 : 0)) * kStep;
-            before = (wave * (steps / kSpanWaves) + min(wave, more)) * kStep;
+        if constexpr (kStep > 1) {
+            // the first waves take the steps that are left over, and of long shares one in
+            // 18 of the others': of the two waves on a SIMD the older is served first and
+            // runs 12% faster (32 sequences of 16K to 32K tokens 131.6 instead of 133.5 us,
+            // 128 of 3000 60.8 instead of 62.5; in 4 bits)
+            const int steps = (u1 - u0 + kStep - 1) / kStep, each = steps / kSpanWaves, more = steps % kSpanWaves;
+            const int extra = each < 12 ? 0 : (each + 8) / 18, first = min(wave, kSpanWaves / 2);
+            share = (each + (wave < kSpanWaves / 2 ? extra : -extra) + (wave < more ? 1 : 0)) * kStep;
+            before = (wave * each + (2 * first - wave) * extra + min(wave, more)) * kStep;
         }
         const int g = u0 + before;
         left = live ? min(share, u1 - g) : 0;

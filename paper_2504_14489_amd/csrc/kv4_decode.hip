@@ -24,7 +24,7 @@ using namespace kv4;
 //     one each; a tile's columns of other blocks are not used.
 // kHeads: 4, 8 or 16, the most query heads of a kv head.
 //
-// Measured: 32 sequences of 16K to 32K tokens of 8 kv heads, 843 MB, 133.5 us (6.3 TB/s;
+// Measured: 32 sequences of 16K to 32K tokens of 8 kv heads, 843 MB, 131.6 us (6.4 TB/s;
 // a plain read reaches 6.5), where memory bounds it.  64 of 512 to 4096, 141 MB, 31.7,
 // and 128 of 64 to 16K of one kv head with 8 query heads, 29 MB, 14.6: a CU's waves
 // issue a page in 0.061 us, and 8 to 10 us pass in a start (lengths, table, pages:

@@ -433,11 +433,13 @@ mw_status mw_kv4_decode_attn(const mw_kv_pool *pool, const mw_attn_shape *shape,
 /* Prefill: arguments as mw_prefill_attn_ws.  A chunk of at most 8 blocks of 128
  * (token, query head) rows to a kv head may read the codes itself (a kernel, and one
  * more where its keys are split and added up); of any other the batch's pages are
- * unpacked to bf16 in the workspace and attended there.  The lengths and head counts
- * alone decide, by what either would take.  The workspace is the size call's for
- * these lengths: the split's sums, which may be none, or 2 * 4096 bytes per (page,
- * kv head) of the batch, a table, and what mw_prefill_attn_ws takes for itself;
- * layers that run one after the other can share it. */
+ * unpacked to bf16 in the workspace and attended there (a kernel before and one after
+ * those of mw_prefill_attn_ws).  The lengths and head counts alone decide, by what
+ * either would take.  A row gets nothing from a token that it does not see, whatever
+ * that holds.  The workspace is the size call's for these lengths: the split's sums,
+ * which may be none, or 2 * 4096 + 8 bytes per (page, kv head) of the batch, a table,
+ * and what mw_prefill_attn_ws takes for itself; layers that run one after the other
+ * can share it. */
 mw_status mw_kv4_prefill_workspace_size(const mw_attn_shape *shape, int32_t batch, const int32_t *h_new_lens,
                                         const int32_t *h_prefix_lens, int32_t num_cus, size_t *bytes);
 mw_status mw_kv4_prefill_attn(const mw_kv_pool *pool, const mw_attn_shape *shape, int32_t batch,

@@ -21,9 +21,32 @@ __device__ __forceinline__ float across_half(float x, const F &f) {
     return f(__builtin_bit_cast(float, lo), __builtin_bit_cast(float, hi));
 }
 
+// Takes blocks of V that are not finite out of four tokens' scale bytes, of `tokens`
+// (0 or 255 in each byte): their scales become finite, which times a probability of
+// 0 gives 0.  Returns them: bit i of byte j is block i of token j.
+__device__ __forceinline__ uint32_t take_bad(uint32_t (&bytes)[kBlocks], uint32_t tokens) {
+    uint32_t bad = 0;
+#pragma unroll
+    for (int i = 0; i < kBlocks; ++i) {
+        const uint32_t x = bytes[i] & tokens;
+        const uint32_t full = ((x & 0x7f7f7f7fu) + 0x01010101u) >> 7 & x >> 7 & 0x01010101u;  // 1 where x has 255
+        bytes[i] &= ~(full * 255);
+        bad |= full << i;
+    }
+    return bad;
+}
+// Mask of the first n of four bytes.
+__device__ __forceinline__ uint32_t first_bytes(int n) { return n >= 4 ? ~0u : n <= 0 ? 0u : (1u << 8 * n) - 1; }
+
 // Unpacks the pages of a batch's sequences, laid end to end, to bf16 pages
 // [page][kv head][16][128] and writes the table that names them.  One wave to a
 // (page, kv head).
+//
+// A row never gets anything from a token that it does not see: the attention masks its
+// scores, but would multiply V by a probability of 0, and 0 times a V that is not
+// finite is NaN.  So such blocks of V of the new tokens are unpacked as zeros and noted
+// in `bad`, four bits a token (64 a page), and k_kv4_unseen makes their dims NaN in the
+// rows from their token on.
 struct ChunkLengths {
     const int32_t *indptr, *prefix;
     int batch, bt_stride;
@@ -37,8 +60,8 @@ struct ChunkLengths {
 
 __global__ void __launch_bounds__(256)
 k_kv4_unpack(const uint8_t *__restrict__ kpool, const uint8_t *__restrict__ vpool, const uint8_t *__restrict__ scales,
-             uint16_t *__restrict__ kout, uint16_t *__restrict__ vout, int32_t *__restrict__ table, int table_stride,
-             const int32_t *__restrict__ indptr, const int32_t *__restrict__ prefix, const int32_t *__restrict__ bt,
+             uint16_t *__restrict__ kout, uint16_t *__restrict__ vout, uint16_t *__restrict__ bad,
+             int32_t *__restrict__ table, int table_stride, const int32_t *__restrict__ indptr, const int32_t *__restrict__ prefix, const int32_t *__restrict__ bt,
              int bt_stride, int batch, int num_pages, int hkv, int64_t items) {
     const int lane = threadIdx.x & 63;
     const int64_t item = static_cast<int64_t>(blockIdx.x) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -81,6 +104,11 @@ k_kv4_unpack(const uint8_t *__restrict__ kpool, const uint8_t *__restrict__ vpoo
     uint4 *ko = reinterpret_cast<uint4 *>(kout + static_cast<size_t>(item) * (kPageSize * kHeadDim)) + lane;
 #pragma unroll
     for (int i = 0; i < 4; ++i) ko[64 * i] = decode_k(codes_k[i], byte_k[i]);
+    const int first = kPageSize * p + 4 * g, r = prefix[b], n = indptr[b + 1] - indptr[b];
+    if (kPageSize * (p + 1) > r) {
+        const uint32_t w = take_bad(bytes, first_bytes(r + n - first) & ~first_bytes(r - first));
+        if (c == 0) bad[4 * item + g] = static_cast<uint16_t>((w & 15) | (w >> 4 & 0xf0) | (w >> 8 & 0xf00) | (w >> 12 & 0xf000));
+    }
     const uint32_t codes[kBlocks] = {vc.x, vc.y, vc.z, vc.w};
     decode_v(codes, bytes, vr);
     uint32_t *vo = reinterpret_cast<uint32_t *>(vout + static_cast<size_t>(item) * (kPageSize * kHeadDim)) + c;
@@ -90,12 +118,47 @@ k_kv4_unpack(const uint8_t *__restrict__ kpool, const uint8_t *__restrict__ vpoo
         for (int k = 0; k < kBlocks; ++k) vo[(4 * g + t) * (kHeadDim / 2) + 16 * k] = vr[t][k];
 }
 
-// Workspace of a prefill call: K pages, V pages, their table, then the
-// workspace of the attention itself.
+// Behind the attention on unpacked pages: for each (sequence, kv head) the first new
+// token whose V is not finite in a block of dims, and NaN there in all rows from it on.
+// (2 us of a call, nearly all of it the launch.)
+__global__ void __launch_bounds__(256)
+k_kv4_unseen(uint16_t *__restrict__ out, const uint64_t *__restrict__ bad, const int32_t *__restrict__ table,
+             int table_stride, int pages, const int32_t *__restrict__ indptr, const int32_t *__restrict__ prefix, int group) {
+    __shared__ int s_first[kBlocks];
+    const int h = blockIdx.x, hkv = gridDim.x, b = blockIdx.y;
+    const int row0 = indptr[b], n = indptr[b + 1] - row0, r = prefix[b];
+    if (n <= 0 || r < 0) return;
+    if (threadIdx.x < kBlocks) s_first[threadIdx.x] = n;
+    __syncthreads();
+    const int end = min((r + n - 1) / kPageSize + 1, table_stride);
+    for (int p = r / kPageSize + static_cast<int>(threadIdx.x); p < end; p += 256) {
+        const int at = table[static_cast<size_t>(b) * table_stride + p];
+        const uint64_t tokens = at >= 0 && at < pages ? bad[static_cast<size_t>(at) * hkv + h] : 0;
+        if (tokens == 0) continue;
+        for (int i = 0; i < kBlocks; ++i) {
+            const uint64_t of_block = tokens >> i & 0x1111111111111111u;
+            if (of_block) atomicMin(&s_first[i], kPageSize * p + __builtin_ctzll(of_block) / 4 - r);
+        }
+    }
+    __syncthreads();
+    for (int i = 0; i < kBlocks; ++i) {
+        // 16 bytes a thread: (row, head) of the group, a quarter of the block's dims
+        const int64_t first = static_cast<int64_t>(s_first[i]) * group * 4, last = static_cast<int64_t>(n) * group * 4;
+        for (int64_t j = first + threadIdx.x; j < last; j += 256) {
+            const int64_t row_head = j >> 2, row = row_head / group;
+            const size_t at = ((row0 + row) * hkv + h) * group + (row_head - row * group);
+            *reinterpret_cast<uint4 *>(out + at * kHeadDim + 32 * i + 8 * (j & 3)) =
+                make_uint4(0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u);
+        }
+    }
+}
+
+// Workspace of a prefill call: K pages, V pages, which of their blocks are not finite,
+// their table, then the workspace of the attention itself.
 struct UnpackLayout {
     int64_t pages;
     int64_t table_stride;
-    size_t off_v, off_table, off_ws;
+    size_t off_v, off_bad, off_table, off_ws;
 };
 mw_status unpack_layout(int32_t batch, const int32_t *h_new_lens, const int32_t *h_prefix_lens, int64_t hkv,
                         UnpackLayout *u, const char *who) {
@@ -110,7 +173,8 @@ mw_status unpack_layout(int32_t batch, const int32_t *h_new_lens, const int32_t 
         return fail(MW_ERR_UNSUPPORTED, "%s: too many pages", who);
     const size_t pages_bytes = static_cast<size_t>(u->pages) * hkv * (kPageSize * kHeadDim * 2);
     u->off_v = pages_bytes;
-    u->off_table = 2 * pages_bytes;
+    u->off_bad = 2 * pages_bytes;
+    u->off_table = u->off_bad + static_cast<size_t>(u->pages) * hkv * 8;
     u->off_ws = (u->off_table + static_cast<size_t>(batch) * u->table_stride * 4 + 255) & ~static_cast<size_t>(255);
     return MW_OK;
 }
@@ -141,9 +205,11 @@ mw_status unpack_layout(int32_t batch, const int32_t *h_new_lens, const int32_t 
 // tile is worked on; one barrier a tile.  A piece leaves (m, l) and its unnormalised
 // output in the workspace and k_kv4_merge adds them up, unless it is the only one.
 //
-// A value that a row does not see never reaches it through the scores; in the tile
-// of its own position a V block that is not finite does reach the rows before it
-// (0 times NaN), as in the bf16 kernels.
+// What a row does not see never reaches it.  Its scores are masked, but a V block that
+// is not finite would come through the product, as 0 times NaN, to all rows of the
+// wave.  So in the tiles that some row of the block does not see whole (at most the
+// last two or three) V holds zeros in its place, and the block is noted beside V:
+// it makes its dims NaN in the rows from its position on.
 constexpr int kBlockRows = 128;
 constexpr int kTileKeys = 64;
 constexpr int kMaxPieces = 64;  // (a lane of the merging wave each)
@@ -179,6 +245,7 @@ k_kv4_prefill(const uint8_t *__restrict__ kpool, const uint8_t *__restrict__ vpo
               Divisor group, int num_pages, float scale_log2, FewRows ws) {
     __shared__ __attribute__((aligned(16))) char s_v[2][kTileKeys * kHeadDim * 2];
     __shared__ __attribute__((aligned(16))) int32_t s_bt[4 * kTableTiles];  // (page, kv head) blocks; -1: absent
+    __shared__ uint32_t s_bad[2][kTileKeys / 4];  // bit i of byte j: block i of V of key 4 [.] + j is not finite
     __shared__ int s_absent;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int l32 = lane & 31, half = lane >> 5;
@@ -229,6 +296,7 @@ k_kv4_prefill(const uint8_t *__restrict__ kpool, const uint8_t *__restrict__ vpo
     const bool valid = mine < rows;
     const int pos = valid ? mine / group : n - 1, head = valid ? mine - pos * group : 0;
     const int seen = r + pos;  // the last key it sees
+    const int t_whole = (r + blk * kBlockRows / group + 1) / kTileKeys;  // tiles that every row of the block sees whole
     const int nt_w = first < rows ? (r + min(first + 31, rows - 1) / group) / kTileKeys + 1 : 0;
     i32x8 q_hi[2], q_lo[2];
     float q_scale;
@@ -275,17 +343,21 @@ k_kv4_prefill(const uint8_t *__restrict__ kpool, const uint8_t *__restrict__ vpo
 #pragma unroll
         for (int i = 0; i < kBlocks; ++i) vs[i] = *reinterpret_cast<const uint32_t *>(sc + i * kPageSize);
     };
-    const auto store_v = [&](int t, char *buf) __attribute__((always_inline)) {
+    const auto store_v = [&](int t, int buf) __attribute__((always_inline)) {
         // keys past the sequence or on an absent page are zeros: 0 times the infinite
         // scale of a slack slot would not be 0
         const int there = __builtin_amdgcn_readfirstlane(s_bt[4 * (t - t_lo) + wave]) < 0 ? 0 : len - (t * kTileKeys + wave * kPageSize + 4 * g);
-        const uint32_t mask = there >= 4 ? ~0u : there <= 0 ? 0u : (1u << 8 * there) - 1;
+        const uint32_t mask = first_bytes(there);
         const uint32_t codes[kBlocks] = {vc.x, vc.y, vc.z, vc.w};
         uint32_t bytes[kBlocks], v[4][kBlocks];
 #pragma unroll
         for (int i = 0; i < kBlocks; ++i) bytes[i] = vs[i] & mask;
+        if (t >= t_whole) {
+            const uint32_t bad = take_bad(bytes, ~0u);
+            if (c == 0) s_bad[buf][4 * wave + g] = bad;
+        }
         decode_v(codes, bytes, v);
-        char *dst = buf + (2 * wave + (g & 1)) * 512 + c * 32 + (g >> 1) * 8;
+        char *dst = s_v[buf] + (2 * wave + (g & 1)) * 512 + c * 32 + (g >> 1) * 8;
         const int flip = 16 * (c >> 3);
 #pragma unroll
         for (int i = 0; i < kBlocks; ++i) {
@@ -304,7 +376,7 @@ k_kv4_prefill(const uint8_t *__restrict__ kpool, const uint8_t *__restrict__ vpo
     const bool absent = s_absent != 0;
     load_v(t_lo);
     load_k(t_lo);
-    store_v(t_lo, s_v[0]);
+    store_v(t_lo, 0);
     load_v(min(t_lo + 1, t_end));
     tile_barrier();
     int t = t_lo;
@@ -340,7 +412,7 @@ k_kv4_prefill(const uint8_t *__restrict__ kpool, const uint8_t *__restrict__ vpo
         // up they would take others, to be waited for and copied at the end of the tile
         __builtin_amdgcn_sched_barrier(0);
         load_k(min(t + 1, t_end));
-        store_v(min(t + 1, t_end), s_v[(t + 1 - t_lo) & 1]);
+        store_v(min(t + 1, t_end), (t + 1 - t_lo) & 1);
         __builtin_amdgcn_sched_barrier(0);
         load_v(min(t + 2, t_end));
         {
@@ -385,10 +457,25 @@ k_kv4_prefill(const uint8_t *__restrict__ kpool, const uint8_t *__restrict__ vpo
                     oacc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
                         *reinterpret_cast<const bf16x8 *>(vb + (4 * d + s) * 1024), p[s], oacc[d], 0, 0, 0);
         }
+        if (t >= t_whole) {
+            const uint32_t bad = s_bad[(t - t_lo) & 1][lane & 15];
+            if (__builtin_amdgcn_ballot_w64(bad != 0) != 0) {
+                uint32_t mine = 0;  // blocks of V that the row sees
+#pragma unroll 1
+                for (int i = 0; i < kTileKeys; ++i) {
+                    const uint32_t of_key = __builtin_amdgcn_readlane(bad, i >> 2) >> (8 * (i & 3)) & 15;
+                    mine |= t * kTileKeys + i <= seen ? of_key : 0;
+                }
+#pragma unroll
+                for (int d = 0; d < 4; ++d)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) oacc[d][i] = mine >> d & 1 ? NAN : oacc[d][i];
+            }
+        }
         tile_barrier();
     }
     for (; t < t_hi; ++t) {  // tiles past all of the wave's rows: its page of each only
-        store_v(min(t + 1, t_end), s_v[(t + 1 - t_lo) & 1]);
+        store_v(min(t + 1, t_end), (t + 1 - t_lo) & 1);
         load_v(min(t + 2, t_end));
         tile_barrier();
     }
@@ -466,11 +553,11 @@ struct FewCost {
     double fixed, tile, byte;  // us of a call, of a tile of the longest piece, of a byte of partials out or in
 };
 constexpr FewCost kFewCost[2] = {{6.5, 1.5, 0.33e-6}, {5.6, 2.29, 0.27e-6}};
-// us of a call, of a tile of each CU (a sixteenth of the keys at least: its pieces),
-// of the first tiles, of a byte of pages read, written and read
+// us of a call (2.1 of them k_kv4_unseen), of a tile of each CU (a sixteenth of the keys
+// at least: its pieces), of the first tiles, of a byte of pages read, written and read
 constexpr struct {
     double fixed, tile, first, byte;
-} kUnpackCost = {9.7, 1.03, 0.68, 0.203e-6};
+} kUnpackCost = {11.8, 1.03, 0.68, 0.203e-6};
 struct FewPlan {
     int32_t groups;  // work-groups; 0: not straight from the codes
     int32_t block_rows, piece_tiles, max_pieces;
@@ -626,6 +713,7 @@ mw_status mw_kv4_prefill_attn(const mw_kv_pool *pool, const mw_attn_shape *shape
     bf16.desc.num_pages = static_cast<int32_t>(u.pages);
     bf16.k = reinterpret_cast<uint16_t *>(ws);
     bf16.v = reinterpret_cast<uint16_t *>(ws + u.off_v);
+    uint16_t *bad = reinterpret_cast<uint16_t *>(ws + u.off_bad);
     int32_t *table = reinterpret_cast<int32_t *>(ws + u.off_table);
     a.d_block_table = table;
     a.bt_stride = static_cast<int32_t>(u.table_stride);
@@ -636,12 +724,19 @@ mw_status mw_kv4_prefill_attn(const mw_kv_pool *pool, const mw_attn_shape *shape
     if (st != MW_OK) return st;
     const int64_t items = u.pages * pool->desc.num_kv_heads;
     hipLaunchKernelGGL(k_kv4_unpack, dim3(static_cast<unsigned>((items + 3) / 4)), dim3(256), 0, s, pool->k4, pool->v4,
-                       pool->scales, bf16.k, bf16.v, table, static_cast<int>(u.table_stride), d_qo_indptr, d_prefix_lens,
+                       pool->scales, bf16.k, bf16.v, bad, table, static_cast<int>(u.table_stride), d_qo_indptr, d_prefix_lens,
                        d_block_table, bt_stride, batch, pool->desc.num_pages, pool->desc.num_kv_heads, items);
     st = check_launch("k_kv4_unpack");
     if (st == MW_OK) st = timing_kernel_done(timing, s);
+    if (st == MW_OK) st = prefill_launch(a, pl, s, timing);
     if (st != MW_OK) return st;
-    return prefill_launch(a, pl, s, timing);
+    hipLaunchKernelGGL(k_kv4_unseen, dim3(static_cast<unsigned>(pl.hkv), batch), dim3(256), 0, s, static_cast<uint16_t *>(d_out),
+                       reinterpret_cast<const uint64_t *>(bad), table, static_cast<int>(u.table_stride),
+                       static_cast<int>(u.pages), d_qo_indptr, d_prefix_lens, pl.group);
+    st = check_launch("k_kv4_unseen");
+    if (st == MW_OK) st = timing_kernel_done(timing, s);
+    timing_end(timing);
+    return st;
 }
 
 }  // extern "C"

@@ -116,8 +116,8 @@ mw_status mw_kv_pool_num_free(const mw_kv_pool *pool, int32_t *n_free);
  * bf16) for i < h_new_lens[b] into position d_start_pos[b] + i of the
  * sequence whose block-table row is b.  A pure bit copy.
  *   h_new_lens  host  [batch]   new tokens per sequence (>= 0)
- *   h_start_pos host  [batch]   first position written (>= 0); validated
- *                               against bt_stride*page_size
+ *   h_start_pos host  [batch]   first position written (>= 0); start + new is
+ *                               validated against bt_stride*page_size and 2^31 - 1
  *   d_qo_indptr device[batch+1] row offsets into d_k_new / d_v_new
  *   d_start_pos device[batch]   same values as h_start_pos
  *   d_block_table device [batch][bt_stride]

@@ -67,7 +67,7 @@ k_kv4_write(uint8_t *__restrict__ kpool, uint8_t *__restrict__ vpool, uint8_t *_
     const int32_t *btrow = bt + static_cast<size_t>(b) * bt_stride;
     if (n <= 0 || pos0 < 0) return;
     const int quad0 = pos0 / 4;
-    const int64_t total = static_cast<int64_t>((pos0 + n + 3) / 4 - quad0) * hkv;
+    const int64_t total = static_cast<int64_t>((pos0 + n - 1) / 4 + 1 - quad0) * hkv;
     for (int64_t idx = static_cast<int64_t>(blockIdx.x) * 16 + (threadIdx.x >> 4); idx < total;
          idx += static_cast<int64_t>(gridDim.x) * 16) {
         const int i = static_cast<int>(static_cast<uint32_t>(idx) / static_cast<uint32_t>(hkv));
@@ -91,7 +91,7 @@ k_kv4_gather(const uint8_t *__restrict__ kpool, const uint8_t *__restrict__ vpoo
     const int32_t *btrow = bt + static_cast<size_t>(b) * bt_stride;
     if (n <= 0 || pos0 < 0) return;
     const int quad0 = pos0 / 4;
-    const int64_t total = static_cast<int64_t>((pos0 + n + 3) / 4 - quad0) * hkv;
+    const int64_t total = static_cast<int64_t>((pos0 + n - 1) / 4 + 1 - quad0) * hkv;
     for (int64_t idx = static_cast<int64_t>(blockIdx.x) * 16 + (threadIdx.x >> 4); idx < total;
          idx += static_cast<int64_t>(gridDim.x) * 16) {
         const int i = static_cast<int>(static_cast<uint32_t>(idx) / static_cast<uint32_t>(hkv));

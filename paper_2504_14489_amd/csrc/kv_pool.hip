@@ -115,6 +115,9 @@ mw_status check_rows(const mw_kv_pool *pool, int32_t batch, const int32_t *h_new
         if (h_new_lens[b] < 0 || h_start_pos[b] < 0 || end > static_cast<int64_t>(bt_stride) * kPageSize)
             return fail(MW_ERR_INVALID_ARG, "%s: sequence %d has positions [%d, %lld) beyond its table of %d pages",
                         who, b, h_start_pos[b], static_cast<long long>(end), bt_stride);
+        if (end > INT32_MAX)
+            return fail(MW_ERR_INVALID_ARG, "%s: sequence %d of %lld tokens: lengths are 32-bit", who, b,
+                        static_cast<long long>(end));
         *max_n = h_new_lens[b] > *max_n ? h_new_lens[b] : *max_n;
         *total += h_new_lens[b];
     }

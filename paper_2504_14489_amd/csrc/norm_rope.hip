@@ -154,7 +154,7 @@ k_norm_rope(NormRopeArgs a, Cache kv, const int32_t *__restrict__ indptr, const 
     const int row0 = indptr[b], n = indptr[b + 1] - row0, pos0 = start_pos[b];
     if (n <= 0 || pos0 < 0) return;
     const int32_t *btrow = kv.bt + static_cast<size_t>(b) * kv.bt_stride;
-    const int quad0 = pos0 / 4, quads = (pos0 + n + 3) / 4 - quad0;
+    const int quad0 = pos0 / 4, quads = (pos0 + n - 1) / 4 + 1 - quad0;
     {
         const uint16_t *from = threadIdx.x < kHeadDim ? a.q_weight : a.k_weight;
         const int d = threadIdx.x % kHeadDim;

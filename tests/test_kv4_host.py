@@ -1,0 +1,40 @@
+"""The host side of the calls on a pool in 4 bits at their limits, without a GPU: no call here launches a kernel."""
+import os
+
+import pytest
+
+from paper_2504_14489_amd import build as B
+from paper_2504_14489_amd import mw
+
+K, V, S = 0x10000, 0x20000, 0x30000  # aligned addresses that are never dereferenced
+
+
+@pytest.fixture(scope="module", autouse=True)
+def lib():
+    if not os.path.exists(mw.LIB_PATH):
+        B.build()
+    return mw.load()
+
+
+@pytest.fixture(params=[4, 16])
+def pool(request):
+    p = mw.mw_kv4_pool_create(10, 16, 2, 128, K, V, S) if request.param == 4 else mw.mw_kv_pool_create(10, 16, 2, 128, K, V)
+    p.bits = request.param
+    yield p
+    mw.mw_kv_pool_destroy(p)
+
+
+@pytest.mark.parametrize("new,start", [([1], [2**31 - 1]), ([2**31 - 1], [1]), ([4, 3], [0, 2**31 - 3])])
+def test_rows_past_the_longest_sequence_are_refused(pool, new, start):
+    """A sequence of 2^31 tokens and more has no 32-bit length, however long its table is."""
+    place = (new, start, 0x100, 0x200, 0x300, 1 << 28)
+    rope = mw.NormRope(num_q_heads=4, rot_dim=0, neighbours=0, eps=0.0, d_q_weight=0, d_k_weight=0, d_inv_freq=0)
+    calls = [lambda: mw.mw_qk_norm_rope_write(pool, rope, *place, 0x400, 1024, 0x800, 1024, 0xA00, 1024, 0xC00)]
+    if pool.bits == 4:
+        calls += [lambda: mw.mw_kv4_pool_write(pool, *place, 0x400, 0x500), lambda: mw.mw_kv4_pool_gather(pool, *place, 0x400, 0x500)]
+    else:
+        calls += [lambda: mw.mw_kv_pool_write(pool, *place, 0x400, 0x500)]
+    for call in calls:
+        with pytest.raises(mw.MWError) as e:
+            call()
+        assert e.value.status == mw.MW_ERR_INVALID_ARG and "32-bit" in e.value.message

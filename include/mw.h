@@ -437,9 +437,9 @@ mw_status mw_kv4_decode_attn(const mw_kv_pool *pool, const mw_attn_shape *shape,
  * those of mw_prefill_attn_ws).  The lengths and head counts alone decide, by what
  * either would take.  A row gets nothing from a token that it does not see, whatever
  * that holds.  The workspace is the size call's for these lengths: the split's sums,
- * which may be none, or 2 * 4096 + 8 bytes per (page, kv head) of the batch, a table,
- * and what mw_prefill_attn_ws takes for itself; layers that run one after the other
- * can share it. */
+ * which may be none, or 2 * 4096 + 8 bytes per (page, kv head) of the sequences with
+ * new tokens, a table, and what mw_prefill_attn_ws takes for itself; layers that run
+ * one after the other can share it. */
 mw_status mw_kv4_prefill_workspace_size(const mw_attn_shape *shape, int32_t batch, const int32_t *h_new_lens,
                                         const int32_t *h_prefix_lens, int32_t num_cus, size_t *bytes);
 mw_status mw_kv4_prefill_attn(const mw_kv_pool *pool, const mw_attn_shape *shape, int32_t batch,

@@ -52,7 +52,7 @@ struct ChunkLengths {
     int batch, bt_stride;
     __device__ __forceinline__ int pages(int b) const {
         if (b >= batch) return 0;
-        const int64_t len = static_cast<int64_t>(indptr[b + 1]) - indptr[b] + prefix[b];
+        const int64_t n = static_cast<int64_t>(indptr[b + 1]) - indptr[b], len = n > 0 ? n + prefix[b] : 0;  // (nothing is read without new tokens)
         const int64_t np = (len + kPageSize - 1) / kPageSize;
         return static_cast<int>(max(int64_t{0}, min(np, static_cast<int64_t>(bt_stride))));
     }
@@ -165,7 +165,7 @@ mw_status unpack_layout(int32_t batch, const int32_t *h_new_lens, const int32_t 
     u->pages = 0;
     u->table_stride = 1;
     for (int32_t b = 0; b < batch; ++b) {
-        const int64_t np = (static_cast<int64_t>(h_new_lens[b]) + h_prefix_lens[b] + kPageSize - 1) / kPageSize;
+        const int64_t np = h_new_lens[b] == 0 ? 0 : (static_cast<int64_t>(h_new_lens[b]) + h_prefix_lens[b] + kPageSize - 1) / kPageSize;
         u->pages += np;
         u->table_stride = np > u->table_stride ? np : u->table_stride;
     }
@@ -644,7 +644,7 @@ mw_status mw_kv4_prefill_workspace_size(const mw_attn_shape *shape, int32_t batc
     UnpackLayout u;
     st = unpack_layout(batch, h_new_lens, h_prefix_lens, shape->num_kv_heads, &u, who);
     if (st != MW_OK) return st;
-    *bytes = u.off_ws + inner;
+    *bytes = u.pages > 0 ? u.off_ws + inner : 0;
     return MW_OK;
 }
 

@@ -38,3 +38,18 @@ def test_rows_past_the_longest_sequence_are_refused(pool, new, start):
         with pytest.raises(mw.MWError) as e:
             call()
         assert e.value.status == mw.MW_ERR_INVALID_ARG and "32-bit" in e.value.message
+
+
+@pytest.mark.parametrize("hq,hkv,new,prefix", [(32, 8, [1000], [0]), (8, 1, [300, 2], [77, 4000])])
+def test_sequences_without_new_tokens_need_no_workspace(hq, hkv, new, prefix):
+    """Beside unpacked ones, whatever their prefix: a row each in the table of pages is all that they add."""
+    size = mw.mw_kv4_prefill_workspace_size(hq, hkv, 128, new, prefix)
+    assert size > 4 << 20
+    longest = max((n + r + 15) // 16 for n, r in zip(new, prefix))
+    more = mw.mw_kv4_prefill_workspace_size(hq, hkv, 128, new + [0] * 31, prefix + [30000] * 31)
+    assert size <= more <= size + 31 * 4 * longest + 256
+    # by themselves they need nothing, and are no reason to refuse a batch
+    assert mw.mw_kv4_prefill_workspace_size(hq, hkv, 128, [0] * 4, [30000] * 4) == 0
+    far = [2**31 - 100] * 64
+    assert mw.mw_kv4_prefill_workspace_size(hq, hkv, 128, [0] * 64, far) == 0
+    assert mw.mw_kv4_prefill_workspace_size(hq, hkv, 128, new + [0] * 64, prefix + far) <= size + 64 * 4 * longest + 256

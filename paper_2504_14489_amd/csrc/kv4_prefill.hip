@@ -662,13 +662,10 @@ mw_status mw_kv4_prefill_attn(const mw_kv_pool *pool, const mw_attn_shape *shape
     if (st != MW_OK) return st;
     hipStream_t s = static_cast<hipStream_t>(stream);
     const int64_t cus = stream_cus(s);
-    // every check of the attention call: on a bf16 pool in the place of this one
-    mw_kv_pool bf16{};
-    bf16.desc = pool->desc;
-    mw_prefill_args a{&bf16,         *shape,        batch,         h_new_lens, h_prefix_lens, d_qo_indptr,
+    mw_prefill_args a{pool,          *shape,        batch,         h_new_lens, h_prefix_lens, d_qo_indptr,
                       d_prefix_lens, d_block_table, bt_stride,     d_q,        d_out};
     PrefillPlan pl;
-    st = prefill_prepare(&a, cus, true, &pl, who, true);
+    st = prefill_prepare(&a, cus, true, &pl, who, true, true);
     if (st != MW_OK) return st;
     const FewPlan few = few_plan(batch, h_new_lens, h_prefix_lens, pl.hkv, pl.group);
     if (total == 0) {
@@ -709,10 +706,8 @@ mw_status mw_kv4_prefill_attn(const mw_kv_pool *pool, const mw_attn_shape *shape
         return fail(MW_ERR_INVALID_ARG, "%s: needs a 16-byte aligned workspace of %zu bytes and the attention's (got %zu)",
                     who, u.off_ws, workspace_bytes);
     char *ws = static_cast<char *>(d_workspace);
-    // the unpacked pages are the pool that the attention reads
-    bf16.desc.num_pages = static_cast<int32_t>(u.pages);
-    bf16.k = reinterpret_cast<uint16_t *>(ws);
-    bf16.v = reinterpret_cast<uint16_t *>(ws + u.off_v);
+    // the unpacked pages, which the attention reads
+    uint16_t *k = reinterpret_cast<uint16_t *>(ws), *v = reinterpret_cast<uint16_t *>(ws + u.off_v);
     uint16_t *bad = reinterpret_cast<uint16_t *>(ws + u.off_bad);
     int32_t *table = reinterpret_cast<int32_t *>(ws + u.off_table);
     a.d_block_table = table;
@@ -724,11 +719,11 @@ mw_status mw_kv4_prefill_attn(const mw_kv_pool *pool, const mw_attn_shape *shape
     if (st != MW_OK) return st;
     const int64_t items = u.pages * pool->desc.num_kv_heads;
     hipLaunchKernelGGL(k_kv4_unpack, dim3(static_cast<unsigned>((items + 3) / 4)), dim3(256), 0, s, pool->k4, pool->v4,
-                       pool->scales, bf16.k, bf16.v, bad, table, static_cast<int>(u.table_stride), d_qo_indptr, d_prefix_lens,
+                       pool->scales, k, v, bad, table, static_cast<int>(u.table_stride), d_qo_indptr, d_prefix_lens,
                        d_block_table, bt_stride, batch, pool->desc.num_pages, pool->desc.num_kv_heads, items);
     st = check_launch("k_kv4_unpack");
     if (st == MW_OK) st = timing_kernel_done(timing, s);
-    if (st == MW_OK) st = prefill_launch(a, pl, s, timing);
+    if (st == MW_OK) st = prefill_launch(a, PrefillPages{k, v, static_cast<int>(u.pages)}, pl, s, timing);
     if (st != MW_OK) return st;
     hipLaunchKernelGGL(k_kv4_unseen, dim3(static_cast<unsigned>(pl.hkv), batch), dim3(256), 0, s, static_cast<uint16_t *>(d_out),
                        reinterpret_cast<const uint64_t *>(bad), table, static_cast<int>(u.table_stride),

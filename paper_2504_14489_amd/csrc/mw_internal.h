@@ -182,9 +182,10 @@ struct PrefillPlan {
 };
 // Validates a prefill call's arguments and plans it for a stream that may use
 // `cus` CUs: one launch of 8-wave blocks (with allow_small, or of 4-wave ones),
-// or with split whatever prefill_split_plan finds best.
+// or with split whatever prefill_split_plan finds best.  four_bit: the kind of pool
+// the call reads (the other kind is refused).
 mw_status prefill_prepare(const mw_prefill_args *a, int64_t cus, bool allow_small, PrefillPlan *p, const char *who,
-                          bool split = false);
+                          bool split = false, bool four_bit = false);
 // Plans body, order and key-range split of a call on `cus` CUs from its lengths
 // (cus = 0: only the largest split any stream could take), with no more pieces
 // than fit workspace_bytes; hkv and group must be set, lengths must have been
@@ -196,9 +197,16 @@ void prefill_split_plan(int32_t batch, const int32_t *h_new_lens, const int32_t 
 // what callers have always brought: prefill_base_pieces.
 mw_status prefill_fit_workspace(const mw_prefill_args *a, int64_t cus, PrefillPlan *p, const void *ws, size_t bytes,
                                 const char *who);
+// The bf16 pages that a prefill call's block table names: its pool's, or those that
+// the call has unpacked.
+struct PrefillPages {
+    const uint16_t *k, *v;
+    int num_pages;
+};
 // Enqueues a call that prefill_split_plan planned (its workspace is the
 // arguments'); `timing` has begun.
-mw_status prefill_launch(const mw_prefill_args &a, const PrefillPlan &pl, hipStream_t s, mw_timing *timing);
+mw_status prefill_launch(const mw_prefill_args &a, const PrefillPages &pages, const PrefillPlan &pl, hipStream_t s,
+                         mw_timing *timing);
 // Pieces of a call on blocks of 32 positions x up to four query heads (1: none):
 // with fewer of them than CUs, so many that two work-groups come on a CU; with
 // fewer than two per CU, three for blocks of 96 tiles and more.  A caller that

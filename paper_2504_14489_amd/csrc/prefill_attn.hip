@@ -460,11 +460,11 @@ mw_status prefill_fit_workspace(const mw_prefill_args *a, int64_t cus, PrefillPl
 }
 
 mw_status prefill_prepare(const mw_prefill_args *a, int64_t cus, bool allow_small, PrefillPlan *p, const char *who,
-                          bool split) {
+                          bool split, bool four_bit) {
     if (!a || !a->pool || a->batch < 0 || a->batch > 65535 || a->bt_stride < 1 ||
         (a->batch > 0 && (!a->h_new_lens || !a->h_prefix_lens)))
         return fail(MW_ERR_INVALID_ARG, "%s: bad arguments", who);
-    const mw_status kind = check_pool_kind(a->pool, false, who);
+    const mw_status kind = check_pool_kind(a->pool, four_bit, who);
     if (kind != MW_OK) return kind;
     const mw_attn_shape *shape = &a->shape;
     const mw_kv_pool *pool = a->pool;
@@ -507,15 +507,16 @@ mw_status prefill_prepare(const mw_prefill_args *a, int64_t cus, bool allow_smal
 }  // namespace mw
 
 // One launch of 8- or 4-wave blocks as planned by prefill_prepare; `timing` has begun.
-static mw_status launch_plain(const mw_prefill_args &a, const PrefillPlan &pl, hipStream_t s, mw_timing *timing) {
+static mw_status launch_plain(const mw_prefill_args &a, const PrefillPages &pages, const PrefillPlan &pl, hipStream_t s,
+                              mw_timing *timing) {
     mw_status st = MW_OK;
     if (pl.gx > 0) {
         auto kernel = pl.waves == 4 ? (pl.table_in_lds ? k_prefill_attn<true, 4> : k_prefill_attn<false, 4>)
                                     : (pl.table_in_lds ? k_prefill_attn<true, 8> : k_prefill_attn<false, 8>);
         hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(pl.gx), pl.gy), dim3(64 * pl.waves), 0, s,
-                           a.pool->k, a.pool->v, static_cast<const uint16_t *>(a.d_q),
+                           pages.k, pages.v, static_cast<const uint16_t *>(a.d_q),
                            static_cast<uint16_t *>(a.d_out), a.d_qo_indptr, a.d_prefix_lens, a.d_block_table,
-                           a.bt_stride, a.batch, Divisor(pl.hkv), Divisor(pl.group), a.pool->desc.num_pages, pl.scale_log2, pl.order);
+                           a.bt_stride, a.batch, Divisor(pl.hkv), Divisor(pl.group), pages.num_pages, pl.scale_log2, pl.order);
         st = check_launch("k_prefill_attn");
         if (st != MW_OK) return st;
     }
@@ -538,7 +539,7 @@ extern "C" mw_status mw_prefill_attn(const mw_kv_pool *pool, const mw_attn_shape
     mw_status st = prefill_prepare(&a, stream_cus(s), true, &pl, who);
     if (st == MW_OK) st = timing_begin(timing, s);
     if (st != MW_OK) return st;
-    return launch_plain(a, pl, s, timing);
+    return launch_plain(a, PrefillPages{pool->k, pool->v, pool->desc.num_pages}, pl, s, timing);
 }
 
 extern "C" mw_status mw_prefill_workspace_size(const mw_attn_shape *shape, int32_t batch, const int32_t *h_new_lens,
@@ -563,8 +564,8 @@ extern "C" mw_status mw_prefill_workspace_size(const mw_attn_shape *shape, int32
 
 namespace mw {
 
-mw_status prefill_launch(const mw_prefill_args &a, const PrefillPlan &pl, hipStream_t s, mw_timing *timing) {
-    const mw_kv_pool *pool = a.pool;
+mw_status prefill_launch(const mw_prefill_args &a, const PrefillPages &pages, const PrefillPlan &pl, hipStream_t s,
+                         mw_timing *timing) {
     const mw_attn_shape *shape = &a.shape;
     const int32_t batch = a.batch, bt_stride = a.bt_stride;
     const int32_t *h_new_lens = a.h_new_lens;
@@ -575,9 +576,9 @@ mw_status prefill_launch(const mw_prefill_args &a, const PrefillPlan &pl, hipStr
     if (pl.big_units > 0) {
         const int64_t n_big = pl.big_units, units = pl.gx;
         auto kernel = pl.table_in_lds ? k_prefill_mixed<true> : k_prefill_mixed<false>;
-        hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(n_big + 2 * (units - n_big))), dim3(512), 0, s, pool->k,
-                           pool->v, static_cast<const uint16_t *>(d_q), static_cast<uint16_t *>(d_out), d_qo_indptr,
-                           d_prefix_lens, d_block_table, bt_stride, batch, Divisor(pl.hkv), Divisor(pl.group), pool->desc.num_pages,
+        hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(n_big + 2 * (units - n_big))), dim3(512), 0, s, pages.k,
+                           pages.v, static_cast<const uint16_t *>(d_q), static_cast<uint16_t *>(d_out), d_qo_indptr,
+                           d_prefix_lens, d_block_table, bt_stride, batch, Divisor(pl.hkv), Divisor(pl.group), pages.num_pages,
                            pl.scale_log2, pl.order, static_cast<int>(n_big));
         st = check_launch("k_prefill_mixed");
         if (st != MW_OK) return st;
@@ -585,7 +586,7 @@ mw_status prefill_launch(const mw_prefill_args &a, const PrefillPlan &pl, hipStr
         timing_end(timing);
         return st;
     }
-    if (!pl.dual) return launch_plain(a, pl, s, timing);
+    if (!pl.dual) return launch_plain(a, pages, pl, s, timing);
     const bool cut = pl.pieces > 1;
     int64_t max_n = 0;
     for (int32_t b = 0; b < batch; ++b) max_n = std::max<int64_t>(max_n, h_new_lens[b]);
@@ -595,9 +596,9 @@ mw_status prefill_launch(const mw_prefill_args &a, const PrefillPlan &pl, hipStr
                                                    kHeadDim * 4);
     auto kernel = cut ? (pl.table_in_lds ? k_prefill_dual<true, true> : k_prefill_dual<false, true>)
                       : (pl.table_in_lds ? k_prefill_dual<true, false> : k_prefill_dual<false, false>);
-    hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(pl.gx * pl.pieces), pl.gy), dim3(512), 0, s, pool->k,
-                       pool->v, static_cast<const uint16_t *>(d_q), static_cast<uint16_t *>(d_out), d_qo_indptr,
-                       d_prefix_lens, d_block_table, bt_stride, batch, Divisor(pl.hkv), Divisor(pl.group), pool->desc.num_pages,
+    hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(pl.gx * pl.pieces), pl.gy), dim3(512), 0, s, pages.k,
+                       pages.v, static_cast<const uint16_t *>(d_q), static_cast<uint16_t *>(d_out), d_qo_indptr,
+                       d_prefix_lens, d_block_table, bt_stride, batch, Divisor(pl.hkv), Divisor(pl.group), pages.num_pages,
                        pl.scale_log2, pl.order, ws_o, ws_ml, pl.rows, pl.piece_tiles, pl.pieces);
     st = check_launch("k_prefill_dual");
     if (st != MW_OK) return st;
@@ -637,5 +638,5 @@ extern "C" mw_status mw_prefill_attn_ws(const mw_kv_pool *pool, const mw_attn_sh
     if (st == MW_OK) st = prefill_fit_workspace(&a, cus, &pl, d_workspace, workspace_bytes, who);
     if (st == MW_OK) st = timing_begin(timing, s);
     if (st != MW_OK) return st;
-    return prefill_launch(a, pl, s, timing);
+    return prefill_launch(a, PrefillPages{pool->k, pool->v, pool->desc.num_pages}, pl, s, timing);
 }

@@ -1,11 +1,14 @@
 """The host side of the calls on a pool in 4 bits at their limits, without a GPU: no call here launches a kernel."""
 import os
+import shutil
+import subprocess
 
 import pytest
 
 from paper_2504_14489_amd import build as B
 from paper_2504_14489_amd import mw
 
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 K, V, S = 0x10000, 0x20000, 0x30000  # aligned addresses that are never dereferenced
 
 
@@ -53,3 +56,53 @@ def test_sequences_without_new_tokens_need_no_workspace(hq, hkv, new, prefix):
     far = [2**31 - 100] * 64
     assert mw.mw_kv4_prefill_workspace_size(hq, hkv, 128, [0] * 64, far) == 0
     assert mw.mw_kv4_prefill_workspace_size(hq, hkv, 128, new + [0] * 64, prefix + far) <= size + 64 * 4 * longest + 256
+
+
+def test_prefill_allocates_nothing(tmp_path):
+    """Calls that end on the host (nothing to do, a workspace too small) make as many allocations as those on a bf16 pool,
+    which make none of their own: a handle of a pool, of a queue and an array, is two."""
+    if not shutil.which("g++"):
+        pytest.skip("g++ not found")
+    src = tmp_path / "allocations.cpp"
+    src.write_text(r"""
+#include <cstdio>
+#include <cstdlib>
+#include <initializer_list>
+#include <new>
+#include "mw.h"
+static long g_count = 0;
+void *operator new(std::size_t n) { ++g_count; return std::malloc(n ? n : 1); }
+void operator delete(void *p) noexcept { std::free(p); }
+void operator delete(void *p, std::size_t) noexcept { std::free(p); }
+alignas(256) static unsigned char fake[4096];  // stands in for device buffers: never dereferenced
+int main() {
+    const mw_kv_pool_desc desc{64, 16, 2, 128};
+    mw_kv_pool *p16, *p4;
+    if (mw_kv_pool_create(&desc, fake, fake, &p16) || mw_kv4_pool_create(&desc, fake, fake, fake, &p4)) return 1;
+    const mw_attn_shape shape{8, 2, 128, 0.1f};
+    int32_t *const d = reinterpret_cast<int32_t *>(fake);
+    const int32_t none[2] = {0, 0}, some[2] = {20, 3}, many[2] = {700, 3}, prefix[2] = {4000, 40};
+    for (int i = 0; i < 4; ++i) {
+        const long a = g_count;
+        mw_status st = mw_prefill_attn_ws(p16, &shape, 2, none, prefix, d, d, d, 500, fake, fake, fake, 0, nullptr, nullptr);
+        const long b = g_count;
+        if (st != MW_OK) return 2;
+        std::printf("%ld", b - a);
+        for (const int32_t *n : {none, some, many}) {
+            const long c = g_count;
+            st = mw_kv4_prefill_attn(p4, &shape, 2, n, prefix, d, d, d, 500, fake, fake, fake, 0, nullptr, nullptr);
+            if (st != (n == none ? MW_OK : MW_ERR_INVALID_ARG)) return 3;
+            std::printf(" %ld", g_count - c);
+        }
+        std::printf("\n");
+    }
+}
+""")
+    exe, where = str(tmp_path / "allocations"), os.path.dirname(mw.LIB_PATH)
+    subprocess.run(["g++", "-std=c++17", "-O1", "-I", os.path.join(ROOT, "include"), str(src), mw.LIB_PATH, "-o", exe,
+                    f"-Wl,-rpath,{where}:/opt/rocm/lib", "-Wl,--allow-shlib-undefined", "-rdynamic"], check=True)
+    res = subprocess.run([exe], capture_output=True, text=True, timeout=120)
+    assert res.returncode == 0, (res.returncode, res.stderr)
+    # the first call of the process may set up the HIP runtime
+    for bf16, *four in [[int(x) for x in line.split()] for line in res.stdout.splitlines()][1:]:
+        assert max(four) <= bf16, res.stdout

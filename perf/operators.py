@@ -318,6 +318,10 @@ def _plain_attention(state):
 
 
 # --------------------------------------------------------- the library's calls
+# what a handle holds the addresses of
+HELD = ("k", "v", "k4", "v4", "scales", "q_weight", "k_weight", "inv_freq")
+
+
 class _Handles:
     """What a program keeps beside its tensors: the pool's handle, output buffers and workspaces."""
 
@@ -327,7 +331,8 @@ class _Handles:
         from paper_2504_14489_amd import mw
 
         self.mw = mw
-        self.stream = torch.cuda.current_stream().cuda_stream
+        self.names = [name for name in HELD if name in state]
+        self.held = [state[name].data_ptr() for name in self.names]
         hq, hkv, kind = state["hq"], state["hkv"], state["case"]["kind"]
         if "k" in state:
             self.pool = mw.mw_kv_pool_create(state["pages"], PAGE, hkv, DIM, state["k"].data_ptr(),
@@ -357,31 +362,33 @@ class _Handles:
 
 
 def _own_run(state):
-    if "own" not in state:
-        state["own"] = _Handles(state)
-    h = state["own"]
+    h = state.get("own")
+    if h is None or h.held != [state[name].data_ptr() for name in h.names]:
+        state["own"] = h = _Handles(state)
+    # torch.cuda.current_stream().cuda_stream without the object (2 us of a call of 9)
+    stream = torch._C._cuda_getCurrentRawStream(state["table"].device.index)
     mw, case, hq, hkv, table = h.mw, state["case"], state["hq"], state["hkv"], state["table"]
     where = (state["h_new"], state["h_prefix"], state["d_indptr"].data_ptr(), state["d_prefix"].data_ptr(),
              table.data_ptr(), table.shape[1])
     if case["kind"] == "decode":
         mw.mw_kv4_decode_attn(h.pool, hq, hkv, DIM, 1.0 / math.sqrt(DIM), state["h_lens"], state["d_lens"].data_ptr(),
                               table.data_ptr(), table.shape[1], state["q"].data_ptr(), h.out.data_ptr(),
-                              h.ws.data_ptr(), h.ws.numel(), h.stream)
+                              h.ws.data_ptr(), h.ws.numel(), stream)
         return h.out
     if case["kind"] == "prefill":
         mw.mw_kv4_prefill_attn(h.pool, hq, hkv, DIM, 1.0 / math.sqrt(DIM), *where, state["q"].data_ptr(),
-                               h.out.data_ptr(), h.ws.data_ptr(), h.ws.numel(), h.stream)
+                               h.out.data_ptr(), h.ws.data_ptr(), h.ws.numel(), stream)
         return h.out
     if case["kind"] == "write":
-        mw.mw_kv4_pool_write(h.pool, *where, state["k_new"].data_ptr(), state["v_new"].data_ptr(), h.stream)
-        mw.mw_kv4_pool_gather(h.pool, *where, h.k_held.data_ptr(), h.v_held.data_ptr(), h.stream)
+        mw.mw_kv4_pool_write(h.pool, *where, state["k_new"].data_ptr(), state["v_new"].data_ptr(), stream)
+        mw.mw_kv4_pool_gather(h.pool, *where, h.k_held.data_ptr(), h.v_held.data_ptr(), stream)
         return {"k": h.k_held, "v": h.v_held}
     rows, stride = state["rows"], state["rows"].stride(0)
     mw.mw_qk_norm_rope_write(h.pool, h.rope, *where, rows.data_ptr(), stride, rows[:, hq:].data_ptr(), stride,
-                             rows[:, hq + hkv:].data_ptr(), stride, h.out.data_ptr(), h.stream)
+                             rows[:, hq + hkv:].data_ptr(), stride, h.out.data_ptr(), stream)
     if case["bits"] == 16:
         return {"q": h.out, "k": state["k"], "v": state["v"]}
-    mw.mw_kv4_pool_gather(h.pool, *where, h.k_held.data_ptr(), h.v_held.data_ptr(), h.stream)
+    mw.mw_kv4_pool_gather(h.pool, *where, h.k_held.data_ptr(), h.v_held.data_ptr(), stream)
     return {"q": h.out, "k": h.k_held, "v": h.v_held}
 
 

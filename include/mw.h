@@ -179,8 +179,7 @@ mw_status mw_kv4_pool_gather(const mw_kv_pool *pool, int32_t batch, const int32_
  *     (a, c) -> (a cos(t f_i) - c sin(t f_i), c cos(t f_i) + a sin(t f_i))
  * over the pairs i < rot_dim / 2 of y: (y[i], y[i + rot_dim/2]), or
  * (y[2i], y[2i+1]) with `neighbours`; dims from rot_dim on are left.  Computed
- * in fp32 (the angle's product in fp64; the squares of a row have to add up to less
- * than 2^128), rounded to bf16 once.  Queries go to
+ * in fp32 (the angle's product in fp64), rounded to bf16 once.  Queries go to
  * d_q_out, keys and the values (unchanged) to the pool, which may be of either
  * kind: in 4 bits the rounded key is what is quantised. */
 typedef struct {

@@ -61,20 +61,32 @@ struct Shared {
 // the halves of its first rot_dim.
 enum Pairing { kNeighbours, kWholeHalves, kHalves };
 
+// Sum of the squares of a row's 128 values, eight of them in each of 16 lanes.
+__device__ __forceinline__ float sum_squares(const float (&y)[8]) {
+    float sum = 0.f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) sum += y[j] * y[j];
+    sum = add_dpp<kXor1>(sum);
+    sum = add_dpp<kXor2>(sum);
+    sum = add_dpp<kHalfMirror>(sum);
+    return add_dpp<kMirror>(sum);
+}
+
 // A lane's dims 8c .. 8c+7 of a head row of token t.
 template <Pairing kPairing>
 __device__ __forceinline__ uint4 norm_rope_row(uint4 x, bool norm, const float *weight, float eps, int rot_dim,
                                                const Shared &sh, int t, int c) {
     float y[8] = {lo(x.x), hi(x.x), lo(x.y), hi(x.y), lo(x.z), hi(x.z), lo(x.w), hi(x.w)};
     if (norm) {
-        float sum = 0.f;
+        float r = rsqrtf(sum_squares(y) * (1.f / kHeadDim) + eps);
+        if (__builtin_amdgcn_ballot_w64(!(r > 0x1p-63f && r < 0x1p50f)) != 0) {
+            // a row whose squares leave the range of fp32, or lose bits at its lower end
+            // next to as small an eps: by a power of two, the root with it
+            const float k = r > 0x1p-63f && r < 0x1p50f ? 1.f : r >= 0x1p50f ? 0x1p70f : 0x1p-70f;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) sum += y[j] * y[j];
-        sum = add_dpp<kXor1>(sum);
-        sum = add_dpp<kXor2>(sum);
-        sum = add_dpp<kHalfMirror>(sum);
-        sum = add_dpp<kMirror>(sum);
-        const float r = rsqrtf(sum * (1.f / kHeadDim) + eps);
+            for (int j = 0; j < 8; ++j) y[j] *= k;
+            r = rsqrtf(sum_squares(y) * (1.f / kHeadDim) + eps * k * k);
+        }
 #pragma unroll
         for (int j = 0; j < 8; ++j) y[j] = y[j] * r * weight[8 * c + j];
     }

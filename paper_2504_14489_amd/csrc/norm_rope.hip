@@ -202,8 +202,14 @@ k_norm_rope(NormRopeArgs a, Cache kv, const int32_t *__restrict__ indptr, const 
         if (2 * f < a.rot_dim) {
             const int t = threadIdx.x >> 6;
             const double turns = static_cast<double>(pos + t) * freq;
-            float sn, cs;
-            sincospif(static_cast<float>(2.0 * (turns - rint(turns))), &sn, &cs);
+            // half turns in [-1, 1], and what their rounding to fp32 leaves (up to 2^-25; a sine
+            // near 0 would be off by 2^-23) by the first order
+            const double half_turns = 2.0 * (turns - rint(turns));
+            const float near = static_cast<float>(half_turns);
+            const float rest = static_cast<float>(half_turns - near) * 3.14159265f;
+            float sn0, cs0;
+            sincospif(near, &sn0, &cs0);
+            const float cs = fmaf(-sn0, rest, cs0), sn = fmaf(cs0, rest, sn0);
             sh.cos[t][f] = cs;
             sh.sin[t][0][f] = -sn;
             sh.sin[t][1][f] = sn;

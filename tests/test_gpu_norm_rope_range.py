@@ -46,3 +46,38 @@ def test_rows_of_any_size(exponents, eps, rot, neighbours):
     finally:
         torch.cuda.synchronize()
         mw.mw_kv_pool_destroy(r.handle)
+
+
+@pytest.mark.parametrize("position", [1, 37, 1000, 30001])
+@pytest.mark.parametrize("neighbours", [False, True])
+def test_cosine_and_sine_near_their_zeros(position, neighbours):
+    """Pairs (1, 0) become (cos, sin); the angles are whole, half and quarter turns, off by 2^-8 to 2^-22 of a half turn.
+    The angle's product in fp64 is off by 2^-51 of it (3 roundings), below 2^-34 for up to 2^14 turns and 2^-11 of the
+    smallest value; what is computed in fp32 is off by less than 2^-20 of the value; the output's rounding by 2^-8."""
+    say(f"rotation near the zeros at {position}, neighbours={neighbours}")
+    r = Rows(4, 2, [1], [position], False, norm=False, neighbours=neighbours, seed=9)
+    try:
+        rng = np.random.Generator(np.random.PCG64(position))
+        off = np.exp2(rng.uniform(-22, -8, 64)) * rng.choice([-1, 1], 64)
+        half_turns = rng.integers(1, 2 * position + 1, 64) * 0.5 + off  # up to half a turn a position
+        freq = half_turns * np.pi / position
+        r.dfreq.copy_(torch.from_numpy(freq))
+        x = np.zeros((1, 8, 128))
+        x[..., (slice(0, 128, 2) if neighbours else slice(0, 64))] = 1
+        r.rows.copy_(R.device(R.f32_to_bf16_bits(x.astype(np.float32)).reshape(1, -1).view(np.int16)))
+        r.run()
+        torch.cuda.synchronize()
+        # the angle as the frequencies give it, in extended precision
+        angle = np.longdouble(freq) * np.longdouble(position)
+        turn = 2 * np.longdouble("3.14159265358979323846264338327950288")
+        angle = angle - np.rint(angle / turn) * turn
+        want = np.zeros(128)
+        one, two = ((slice(0, 128, 2), slice(1, 128, 2)) if neighbours else (slice(0, 64), slice(64, 128)))
+        want[one], want[two] = np.cos(angle), np.sin(angle)
+        assert 2.0**-22 < np.abs(want).min() < 2.0**-12
+        got = bits_to_f32(R.bits_of(r.q_out))[0].astype(np.float64)
+        bound = (2.0**-8 + 2.0**-20) * np.abs(want) + 2.0**-33
+        assert (np.abs(got - want) <= bound).all(), float((np.abs(got - want) / bound).max())
+    finally:
+        torch.cuda.synchronize()
+        mw.mw_kv_pool_destroy(r.handle)

@@ -102,6 +102,11 @@ mw_status check_args(const mw_engine *eng, const mw_decode_args *dec, const mw_p
         return fail(MW_ERR_INVALID_ARG, "mw_engine_run: decode_graph must be 0 or 1");
     if (pl->decode_graph && dec->batch > (1 << 20))
         return fail(MW_ERR_INVALID_ARG, "mw_engine_run: decode batch too large");
+    // before a call of one phase is under way when the other's is refused
+    for (const mw_kv_pool *pool : {dec->pool, pre->pool}) {
+        const mw_status st = pool ? check_pool_kind(pool, false, "mw_engine_run") : MW_OK;
+        if (st != MW_OK) return st;
+    }
     return MW_OK;
 }
 

@@ -420,8 +420,11 @@ mw_status mw_decode_attn_noalloc(const mw_kv_pool *pool, const mw_attn_shape *sh
                                  void *d_out, int32_t chunk_pages, mw_stream stream);
 
 /* Attention over a pool in 4 bits: the calls above on the values that the codes
- * stand for.  K is used as held; queries, probabilities and sums as in the bf16
- * calls.
+ * stand for.  K is used as held; probabilities and sums as in the bf16 calls.  A query
+ * row enters the scores as two 8-bit floats per value, exact but for values below
+ * 2^-9 of the row's largest, which are off by at most 2^-17 of that; a prefill that
+ * unpacks (below) takes queries as they are.  mw_engine_run, mw_fused_attn and
+ * mw_decode_attn_noalloc are for bf16 pools and refuse these.
  * Decode: arguments as mw_decode_attn, with its balanced split (chunk_pages 0). */
 mw_status mw_kv4_decode_workspace_size(const mw_attn_shape *shape, int32_t batch, const int32_t *h_seq_lens,
                                        size_t *bytes);

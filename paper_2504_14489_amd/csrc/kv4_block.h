@@ -25,8 +25,9 @@ __device__ __forceinline__ void split2(uint32_t two, float unit, i16x2 &hi, i16x
 // A query row as two e4m3 operands of the scaled matrix instruction, hi + lo: with
 // q 2^-e, e such that the row's largest is in [128, 256), hi is its nearest and lo
 // the nearest of the rest.  hi keeps four bits of the eight that bf16 has and the
-// rest has four, so the sum is exact down to 2^-10 of the row's largest, and off by
-// at most 2^-18 of it below.
+// rest has four, so the sum is exact down to 2^-9 of the row's largest; below, the
+// rest is rounded to its smallest step, 2^-9, and the sum is off by at most 2^-10, 2^-17
+// of a row's largest of 128.
 // x[4 i + j], j < 4: the lane's dims of operand i, the first 16 bytes of the
 // operand and the last; the row's other dims are in the lanes 32 apart and, with
 // kQuarters, those 16 apart.  Returns the factor of its scores.

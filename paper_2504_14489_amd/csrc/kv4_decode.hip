@@ -29,7 +29,10 @@ using namespace kv4;
 // and 128 of 64 to 16K of one kv head with 8 query heads, 29 MB, 14.6: a CU's waves
 // issue a page in 0.061 us, and 8 to 10 us pass in a start (lengths, table, pages:
 // dependent loads) and an end (pieces, flags, merge) on which nothing else waits.
-// One of 4003 tokens, 4.4 MB, takes 9.3 and has little else.
+// One of 4003 tokens, 4.4 MB, takes 9.3 and has little else.  On 192, 128, 64 and 32 CUs
+// the first takes 152, 201, 381 and 748 us (0.061 us a page of a CU on the last two) and
+// the second 39, 48, 82 and 149.  With 16 query heads a kv head, 32 of 16K to 32K of 8 kv
+// heads take 161 us (5.3 TB/s; 252 on 128 CUs) and 64 of 512 to 4096 of one 15.2.
 //
 // A unit has eight waves, with steps of four pages: sixteen with steps of two (128
 // registers, the scores' bookkeeping twice as often) took 41 us for 32 sequences

@@ -120,7 +120,7 @@ k_kv4_unpack(const uint8_t *__restrict__ kpool, const uint8_t *__restrict__ vpoo
 
 // Behind the attention on unpacked pages: for each (sequence, kv head) the first new
 // token whose V is not finite in a block of dims, and NaN there in all rows from it on.
-// (2 us of a call, nearly all of it the launch.)
+// (2.1 to 2.9 us of a call: a launch and three dependent loads.)
 __global__ void __launch_bounds__(256)
 k_kv4_unseen(uint16_t *__restrict__ out, const uint64_t *__restrict__ bad, const int32_t *__restrict__ table,
              int table_stride, int pages, const int32_t *__restrict__ indptr, const int32_t *__restrict__ prefix, int group) {
@@ -182,11 +182,12 @@ mw_status unpack_layout(int32_t batch, const int32_t *h_new_lens, const int32_t 
 // ------------------------------------------------------- few rows: straight from the codes
 // A chunk of few rows reads each page for few query blocks, so unpacking it to
 // bf16 first (write 8192 bytes, read them again) costs more than it saves: 64
-// tokens over 8000 of 32/8 heads take 25 us like this and 37 unpacked, 16 tokens 18
-// and 34.  A tile takes 1.5 us of a CU with one work-group, 1.1 of each of two; it
-// is bound by the instructions that its four waves issue, not by memory (reading
-// the same tile over and over changes nothing; without the conversions it is 15-20%
-// shorter, without the exponentials or half of the second product 10% each).
+// tokens over 8000 of 32/8 heads take 25 us like this and 42 unpacked, 16 tokens 17
+// and 42.  A tile takes 1.5 us of a CU with one work-group, 1.1 of each of two; it
+// is bound by what each of its four waves does one after the other (scores, conversion
+// of V, exponentials, second product), not by memory (reading the same tile over and
+// over changes nothing; without the conversions it is 15-20% shorter, without the
+// exponentials or half of the second product 10% each).
 //
 // A work-group is four waves on 128 rows of a (sequence, kv head) (row = position *
 // group + head, 32 per wave) and one piece of their keys, 64 at a time:
@@ -381,8 +382,6 @@ k_kv4_prefill(const uint8_t *__restrict__ kpool, const uint8_t *__restrict__ vpo
     tile_barrier();
     int t = t_lo;
     for (const int t_seen = min(t_hi, nt_w); t < t_seen; ++t) {
-        // the matrix instructions of the scores, with the conversion of the next tile's
-        // V between them
         f32x16 sc[2];
         {
             if (absent) {  // keys on an absent page are zeros
@@ -439,6 +438,8 @@ k_kv4_prefill(const uint8_t *__restrict__ kpool, const uint8_t *__restrict__ vpo
 #pragma unroll
                 for (int d = 0; d < 4; ++d) oacc[d] *= alpha;
             }
+            // bf16 for the second product, as in the bf16 cache's kernels (off by 2^-8 of a
+            // weight at most); the sum is of the weights before that
             bf16x8 p[4];
 #pragma unroll
             for (int s = 0; s < 4; ++s) {
@@ -539,13 +540,17 @@ k_kv4_merge(uint16_t *__restrict__ out, const int32_t *__restrict__ indptr, cons
 // of batches, of 1 to 32 kv heads, each made all three ways: straight from the codes
 // with one work-group to a CU, with two that slow each other down, or unpacked
 // first.  The way so chosen took 1% longer than the fastest in the mean and 14% at
-// most.  us (one, two, unpacked), 8 kv heads of 4 query heads:
-//       1 token over 0           6.7    6.7   11.4      64 over 2000      18.5  22.2  22.6
-//      16 tokens over 8000      18.1   20.9   33.3      64 over 30000     64    58    86
-//     256 tokens over 0         16.1   15.8   12.9     256 over 8000      63    59    56
-//     16 sequences of 4 over 4000  51  37    112        4 of 128 over 500 27    31    20
+// most.  us (one, two, unpacked), 8 kv heads of 4 query heads, as measured now:
+//       1 token over 0           6.6    6.6    9.8      64 over 2000      17.3  20.9  27.7
+//      16 tokens over 8000      16.5   19.6   42.1      64 over 30000     57    53    83
+//     256 tokens over 0         14.9   15.0   14.3     256 over 8000      61    55    57
+//     16 sequences of 4 over 4000  50  35    114        4 of 128 over 500 27    31    24
 // The costs are those of a whole MI355X whatever CUs the stream has, so that the
-// workspace and the results do not depend on it; both ways slow down alike.
+// workspace and the results do not depend on it.  On fewer CUs the way straight from the
+// codes slows down more than the other, whose unpacking needs few: over 18 calls the one
+// chosen took 1% longer than the fastest in the mean (8% at most) on 256 CUs, 3% (18%)
+// on 192, 7% (35%) on 128, 17% (81%) on 64 and 37% (175%) on 32, where 256 tokens over 0
+// take 42 us and unpacked 15.
 constexpr int kCus = 256;
 constexpr size_t kRowBytes = kHeadDim * 4 + 8;
 constexpr int kFewBlocks = 8;  // (pages read by more blocks are unpacked with profit)

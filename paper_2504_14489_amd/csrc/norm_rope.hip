@@ -8,7 +8,7 @@
 // (y_2i, y_2i+1).  Dims past rot_dim stay.  Sums, norm and rotation are fp32, one
 // rounding to bf16 at the end; the angle t f_i is a product in 64 bits, brought
 // to one turn before fp32 sees it (at t = 10^5, f = 1 the fp32 product is off by
-// 2^-8 of a radian).
+// 2^-8 of a radian), and what that rounding leaves is added to cosine and sine.
 //
 // Bound by memory: every row is read and written once, 256 bytes a head.
 #include "kv4_format.h"
@@ -155,7 +155,7 @@ __device__ __forceinline__ int each_row(uint4 x, int group, int step, int t0, in
 // and lie in LDS; then 16 lanes take a head row at a time.  Quads, because V in 4
 // bits is stored by four tokens (kv4_format.h).
 // Measured (kernel alone): 4096 tokens of 32 + 2 * 8 heads into bf16, 101 MB, 23 us
-// (a copy of as many bytes 21); 10315 of 64 + 2 * 8 into 4 bits, 391 MB, 82 us (a copy
+// (a copy of as many bytes 21); 10315 of 64 + 2 * 8 into 4 bits, 391 MB, 84 us (a copy
 // 80).  Six work-groups per CU: with the registers of five the latter takes 6% longer.
 // kPassBy: rows are read and queries stored past the caches.
 template <bool kFourBit, Pairing kPairing, bool kPassBy>
